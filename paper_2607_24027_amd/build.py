@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsolattn.so")
-SOURCES = ["sol_attn_kernels.hip", "sol_attn_baselines.hip", "sol_attn_noalloc.hip", "sol_attn_api.cpp"]
+SOURCES = ["sol_attn_kernels.hip", "sol_attn_baselines.hip", "sol_attn_noalloc.hip", "sol_attn_api.cpp",
+           "sol_cache.hip", "sol_cache_attn.hip", "sol_cache_api.cpp"]
 ARCH = os.environ.get("SOL_ATTN_ARCH", "gfx950")
 
 
@@ -34,9 +35,10 @@ def build(verbose: bool = False) -> str:
     os.makedirs(build_dir, exist_ok=True)
     for src in SOURCES:
         obj = os.path.join(build_dir, src + ".o")
-        # Kernels never see NaN by contract (NaN inputs are invalid); this lets max() skip
-        # NaN canonicalisation of MFMA results.  Infinities keep their IEEE meaning.
-        extra = ["-fno-honor-nans"] if src.endswith(".hip") else []
+        # The forward kernels never see NaN by contract (NaN inputs are invalid); this lets max() skip
+        # NaN canonicalisation of MFMA results.  Infinities keep their IEEE meaning.  The serving operators carry
+        # NaN of a token to the rows that see it.
+        extra = ["-fno-honor-nans"] if src.endswith(".hip") and not src.startswith("sol_cache") else []
         cmd = [hipcc(), "-x", "hip", *common, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
         _run(cmd, verbose)
         objs.append(obj)

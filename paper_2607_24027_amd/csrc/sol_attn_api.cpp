@@ -169,6 +169,15 @@ int validate_forward(const void* q, const void* k, const void* v, const void* ou
 
 }  // namespace
 
+namespace sol {
+
+int set_error(int code, const char* text) {
+    g_err = text;
+    return code;
+}
+
+}  // namespace sol
+
 extern "C" {
 
 const char* sol_attn_last_error(void) { return g_err.c_str(); }

@@ -1,0 +1,486 @@
+// Serving operators around the 4-bit cache: norm and rotation of queries and keys, page tables, append and
+// read-back.  The attention over the cache is in sol_cache_attn.hip.
+#include "sol_cache_internal.h"
+
+#include <algorithm>
+#include <climits>
+
+namespace sol {
+namespace {
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf16_to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+// Round to nearest even; NaN stays NaN.
+__device__ __forceinline__ uint32_t f32_to_bf16(float x) {
+    const uint32_t b = __float_as_uint(x);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return (b >> 16) | 0x40u;
+    return (b + 0x7fffu + ((b >> 16) & 1u)) >> 16;
+}
+
+struct BF16 {
+    static constexpr int size = 2;
+};
+struct F32 {
+    static constexpr int size = 4;
+};
+
+// Four consecutive elements at element offset `at` of p.  VEC: p and `at` are multiples of 8 bytes (bf16) or 16 bytes (f32).
+template <class E, bool VEC>
+__device__ __forceinline__ f32x4 load4(const void* p, long long at) {
+    f32x4 r;
+    if constexpr (E::size == 2) {
+        const uint16_t* x = static_cast<const uint16_t*>(p) + at;
+        if constexpr (VEC) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(x);
+            r[0] = __uint_as_float(w[0] << 16);
+            r[1] = __uint_as_float(w[0] & 0xffff0000u);
+            r[2] = __uint_as_float(w[1] << 16);
+            r[3] = __uint_as_float(w[1] & 0xffff0000u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = bf16_to_f32(x[i]);
+        }
+    } else {
+        const float* x = static_cast<const float*>(p) + at;
+        if constexpr (VEC) {
+            r = *reinterpret_cast<const f32x4*>(x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = x[i];
+        }
+    }
+    return r;
+}
+
+template <class E, bool VEC>
+__device__ __forceinline__ void store4(void* p, long long at, f32x4 r) {
+    if constexpr (E::size == 2) {
+        uint16_t* x = static_cast<uint16_t*>(p) + at;
+        const uint32_t a = f32_to_bf16(r[0]), b = f32_to_bf16(r[1]), c = f32_to_bf16(r[2]), d = f32_to_bf16(r[3]);
+        if constexpr (VEC) {
+            *reinterpret_cast<u32x2*>(x) = u32x2{a | (b << 16), c | (d << 16)};
+        } else {
+            x[0] = (uint16_t)a, x[1] = (uint16_t)b, x[2] = (uint16_t)c, x[3] = (uint16_t)d;
+        }
+    } else {
+        float* x = static_cast<float*>(p) + at;
+        if constexpr (VEC) {
+            *reinterpret_cast<f32x4*>(x) = r;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = r[i];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Norm and rotation.  D / 8 lanes hold a head of a token, each two runs of four channels, so that both members of every
+// rotated pair are in one lane: with halves lane i < rot/8 holds the runs i and i + rot/8 (of four channels), the other
+// lanes consecutive runs of what is not rotated; with pairs lane i holds the runs 2i and 2i + 1.  A thread keeps its
+// token's cosines and sines for the heads [h0, h0 + heads) it goes through.  blockIdx.x: tokens, blockIdx.y: heads of q and k.
+// ---------------------------------------------------------------------------
+template <class E, int D, bool VEC>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(const RopeArgs a, const int heads) {
+    constexpr int LPR = D / 8, ROWS = 256 / LPR;
+    const int lane = threadIdx.x % LPR;
+    const long long t = (long long)blockIdx.x * ROWS + threadIdx.x / LPR;
+    if (t >= (long long)a.B * a.N) return;
+    const int b = (int)(t / a.N), n = (int)(t % a.N);
+    const int quads = a.rot / 8;   // rotated runs of four in each half
+    const bool turned = lane < quads;
+    int c0, c1;
+    if (a.pairs) {
+        c0 = 8 * lane, c1 = c0 + 4;
+    } else if (turned) {
+        c0 = 4 * lane, c1 = c0 + a.rot / 2;
+    } else {
+        c0 = 8 * lane, c1 = c0 + 4;   // quads lanes hold 8 quads channels: the others go on at 8 quads
+    }
+    int pos = n;
+    if (a.positions) pos = a.positions[t];
+    if (pos < 0 || (a.rot > 0 && pos >= a.P)) return;   // uniform over the lanes of a row
+    f32x4 cs = {1.f, 1.f, 1.f, 1.f}, sn = {0.f, 0.f, 0.f, 0.f};
+    if (turned) {
+        const long long at = (long long)pos * (a.rot / 2) + 4 * lane;
+        cs = load4<F32, VEC>(a.cos, at);
+        sn = load4<F32, VEC>(a.sin, at);
+    }
+    auto weights = [&](const void* w, f32x4& w0, f32x4& w1) {
+        w0 = w1 = f32x4{1.f, 1.f, 1.f, 1.f};
+        if (!w) return;
+        if (a.wdtype == 0) {
+            w0 = load4<BF16, VEC>(w, c0);
+            w1 = load4<BF16, VEC>(w, c1);
+        } else {
+            w0 = load4<F32, VEC>(w, c0);
+            w1 = load4<F32, VEC>(w, c1);
+        }
+    };
+    const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, a.Hq + a.Hk);
+    auto part = [&](const void* x, void* y, const Strides& sx, const Strides& sy, const void* w, int lo, int hi) {
+        if (lo >= hi) return;
+        f32x4 w0, w1;
+        weights(w, w0, w1);
+        const long long xi = b * sx.b + n * sx.n, yi = b * sy.b + n * sy.n;
+#pragma unroll 2
+        for (int h = lo; h < hi; ++h) {
+            f32x4 x0 = load4<E, VEC>(x, xi + h * sx.h + c0), x1 = load4<E, VEC>(x, xi + h * sx.h + c1);
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ss += x0[i] * x0[i] + x1[i] * x1[i];
+#pragma unroll
+            for (int m = 1; m < LPR; m *= 2) ss += __shfl_xor(ss, m);
+            const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+            x0 = x0 * r * w0, x1 = x1 * r * w1;
+            f32x4 y0, y1;
+            if (a.pairs) {
+                y0[0] = x0[0] * cs[0] - x0[1] * sn[0], y0[1] = x0[1] * cs[0] + x0[0] * sn[0];
+                y0[2] = x0[2] * cs[1] - x0[3] * sn[1], y0[3] = x0[3] * cs[1] + x0[2] * sn[1];
+                y1[0] = x1[0] * cs[2] - x1[1] * sn[2], y1[1] = x1[1] * cs[2] + x1[0] * sn[2];
+                y1[2] = x1[2] * cs[3] - x1[3] * sn[3], y1[3] = x1[3] * cs[3] + x1[2] * sn[3];
+            } else {
+                y0 = x0 * cs - x1 * sn;
+                y1 = x1 * cs + x0 * sn;
+            }
+            store4<E, VEC>(y, yi + h * sy.h + c0, y0);
+            store4<E, VEC>(y, yi + h * sy.h + c1, y1);
+        }
+    };
+    part(a.q, a.qo, a.sq, a.sqo, a.wq, min(h0, a.Hq), min(h1, a.Hq));
+    part(a.k, a.ko, a.sk, a.sko, a.wk, max(h0, a.Hq) - a.Hq, h1 - a.Hq);
+}
+
+// ---------------------------------------------------------------------------
+// Page tables.  Every workgroup scans the lengths (at most four requests a thread) into shared memory; then the new table
+// entries and the rows are dealt to all workgroups by binary searches in the sums, and the first one writes what there is once.
+// New entries lie behind the used part of a table row and in front of the ring, pages that come back behind the ring's
+// last: no workgroup reads what another writes.
+// ---------------------------------------------------------------------------
+constexpr int kTablesThreads = 1024, kTablesRows = 4096;
+
+// First index with sum[i] > x, of n ascending sums.
+__device__ __forceinline__ int upper_bound(const int* sum, int n, int x) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (sum[mid] > x) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+__global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const TablesArgs a) {
+    __shared__ int s_rows[kMaxRequests], s_need[kMaxRequests], s_gone[kMaxRequests];   // inclusive sums
+    __shared__ int s_len[kMaxRequests];                                                // held length; ~length: refused
+    __shared__ long long w_rows[16];
+    __shared__ int w_need[16], w_gone[16], s_taken;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int S = a.S, MP = a.max_pages, P = a.P;
+    const long long room = (long long)MP * kPage;
+    const int head = ((a.state[0] % P) + P) % P, count = min(max(a.state[1], 0), P);
+    if (tid == 0) s_taken = 0;
+    // thread tid owns requests [e0, e1)
+    const int per = (S + kTablesThreads - 1) / kTablesThreads;
+    const int e0 = min(tid * per, S), e1 = min(e0 + per, S);
+    long long rows = 0;
+    int need = 0, gone = 0;
+    auto step = [&](int s, long long& r, int& nd, int& gn, int& len, long long& want, bool& full) {
+        len = (int)min((long long)max(a.lens[s], 0), room);
+        const long long add = a.add[s];
+        r = max(add, 0ll);
+        full = add > 0 && len + add > room;
+        want = full ? len : max(len + add, 0ll);
+        const int before = (len + kPage - 1) / kPage, after = (int)((want + kPage - 1) / kPage);
+        nd = max(after - before, 0);
+        gn = max(before - after, 0);
+    };
+    for (int s = e0; s < e1; ++s) {
+        long long r, want;
+        int nd, gn, len;
+        bool full;
+        step(s, r, nd, gn, len, want, full);
+        rows += r, need += nd, gone += gn;
+    }
+    long long rows_in = rows;
+    int need_in = need, gone_in = gone;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const long long x = __shfl_up(rows_in, m);
+        const int y = __shfl_up(need_in, m), z = __shfl_up(gone_in, m);
+        if (lane >= m) rows_in += x, need_in += y, gone_in += z;
+    }
+    if (lane == 63) w_rows[wave] = rows_in, w_need[wave] = need_in, w_gone[wave] = gone_in;
+    __syncthreads();
+    rows_in -= rows, need_in -= need, gone_in -= gone;
+    for (int w = 0; w < wave; ++w) rows_in += w_rows[w], need_in += w_need[w], gone_in += w_gone[w];
+    for (int s = e0; s < e1; ++s) {
+        long long r, want;
+        int nd, gn, len;
+        bool full;
+        step(s, r, nd, gn, len, want, full);
+        rows_in += r, need_in += nd, gone_in += gn;
+        const bool granted = !full && (nd == 0 || need_in <= count);
+        const int row_end = (int)min(rows_in, (long long)INT_MAX);
+        s_rows[s] = row_end;
+        s_need[s] = need_in;
+        s_gone[s] = gone_in;
+        s_len[s] = granted ? len : ~len;
+        if (granted && nd > 0) atomicMax(&s_taken, need_in);   // the largest of the granted sums, whatever the order
+        if (blockIdx.x == 0) {
+            a.lens_out[s] = granted ? (int)want : len;
+            a.row_start[s + 1] = row_end;
+        }
+    }
+    if (blockIdx.x == 0 && tid == 0) a.row_start[0] = 0;
+    __syncthreads();
+    const int taken = s_taken;
+    auto held = [&](int s) { return s_len[s] < 0 ? ~s_len[s] : s_len[s]; };
+    auto fresh = [&](int rank) { return a.ring[(int)(((long long)head + rank) % P)]; };
+    for (int r = blockIdx.x * kTablesThreads + tid; r < taken; r += gridDim.x * kTablesThreads) {
+        const int s = upper_bound(s_need, S, r);
+        const int page = (held(s) + kPage - 1) / kPage + r - (s ? s_need[s - 1] : 0);
+        a.table[(long long)s * MP + page] = fresh(r);
+    }
+    const int total_rows = s_rows[S - 1];
+    for (int t = blockIdx.x * kTablesRows + tid; t < min(a.rows, (int)(blockIdx.x + 1) * kTablesRows); t += kTablesThreads) {
+        int slot = -1, pos = -1;
+        if (t < total_rows) {
+            const int s = upper_bound(s_rows, S, t);
+            if (s_len[s] >= 0) {
+                const int len = s_len[s], used = (len + kPage - 1) / kPage;
+                pos = len + t - (s ? s_rows[s - 1] : 0);
+                const int p = pos / kPage;
+                const int page = p < used ? a.table[(long long)s * MP + p] : fresh((s ? s_need[s - 1] : 0) + p - used);
+                slot = page >= 0 && page < P ? page * kPage + pos % kPage : -1;
+            }
+        }
+        a.slots[t] = slot;
+        a.positions[t] = pos;
+    }
+    if (blockIdx.x) return;
+    // Pages that come back, in order: the valid ones of 1,024 entries at a time.
+    const int total_gone = s_gone[S - 1];
+    int base = 0;
+    for (int r0 = 0; r0 < total_gone; r0 += kTablesThreads) {
+        const int r = r0 + tid;
+        int page = -1;
+        if (r < total_gone) {
+            const int s = upper_bound(s_gone, S, r);
+            const int before = (held(s) + kPage - 1) / kPage;
+            page = a.table[(long long)s * MP + before - (s_gone[s] - r)];
+        }
+        const bool valid = page >= 0 && page < P;
+        const uint64_t m = __ballot(valid);
+        __syncthreads();
+        if (lane == 0) w_need[wave] = __popcll(m);
+        __syncthreads();
+        int rank = base + __popcll(m & ((1ull << lane) - 1));
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) rank += w_need[w];
+            base += w_need[w];
+        }
+        if (valid && rank < P - count) a.ring[(int)(((long long)head + count + rank) % P)] = page;
+    }
+    if (tid == 0) {
+        a.state_out[0] = (int)(((long long)head + taken) % P);
+        a.state_out[1] = count - taken + min(base, P - count);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Append.  D / 4 lanes hold a token of a head, half of them its key and half its value, eight channels each; four
+// lanes share a scale.
+// ---------------------------------------------------------------------------
+template <int D>
+__device__ __forceinline__ int k_scale_at(int tok, int group) {   // byte of a group's scale inside the key scales
+    const int t = tok & 31, swapped = (t & 19) | ((t & 4) << 1) | ((t & 8) >> 1);
+    return (((group & 1) * 32 + swapped) * (D / 64) + (group >> 1)) * 2 + (tok >> 5);
+}
+
+template <class E, int D, bool VEC>
+__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
+    using L = PageLayout<D>;
+    constexpr int LPT = D / 4, HALF = LPT / 2;
+    const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LPT;
+    const int sub = threadIdx.x % LPT, piece = sub % HALF;
+    const bool is_v = sub >= HALF;
+    if (item >= (long long)a.T * a.H) return;   // whole groups of LPT lanes
+    const int t = (int)(item / a.H), h = (int)(item % a.H);
+    const int slot = a.slots[t];
+    if (slot < 0 || slot / kPage >= a.P) return;
+    const Strides& st = is_v ? a.sv : a.sk;
+    const void* src = is_v ? a.v : a.k;
+    const long long at = h * st.h + t * st.n + 8 * piece;
+    const f32x4 x0 = load4<E, VEC>(src, at), x1 = load4<E, VEC>(src, at + 4);
+    uint32_t top = 0;   // magnitudes order as integers, NaN above infinity
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        top = max(top, __float_as_uint(x0[i]) & 0x7fffffffu);
+        top = max(top, __float_as_uint(x1[i]) & 0x7fffffffu);
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    int bad = top >= 0x7f800000u;
+#pragma unroll
+    for (int m = 4; m < LPT; m *= 2) bad |= __shfl_xor(bad, m);
+    // floor(log2 m) - 2, one more past 7/4 of the power of two: adding 2^21 - 1 to the bits carries from 1.75 + 1 ulp on
+    int e = (int)((top + 0x1fffffu) >> 23) - 127 - 2;
+    e = is_v ? min(max(e, -23), 13) : min(max(e, -100), 125);
+    const float scale = __uint_as_float((uint32_t)(e + 127) << 23);
+    uint32_t code = 0;
+    if (!bad) {
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x0[0], x0[1], scale, 0);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x0[2], x0[3], scale, 1);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x1[0], x1[1], scale, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x1[2], x1[3], scale, 3);
+    }
+    uint8_t* page = a.store + ((long long)(slot / kPage) * a.H + h) * L::bytes;
+    const int tok = slot % kPage, group = piece >> 2;
+    const uint8_t byte = bad && !is_v ? 255 : (uint8_t)(e + 127);
+    if (!is_v) {
+        *reinterpret_cast<uint32_t*>(page + L::k + tok * (D / 2) + 4 * piece) = code;
+        if ((piece & 3) == 0) page[L::ks + k_scale_at<D>(tok, group)] = byte;
+    } else {
+        uint8_t* to = page + L::v + ((tok >> 3) * 32 * 8 + (tok & 7)) * (D / 64);
+        if constexpr (D == 128) {
+            *reinterpret_cast<uint16_t*>(to + (2 * piece) * 16) = (uint16_t)code;
+            *reinterpret_cast<uint16_t*>(to + (2 * piece + 1) * 16) = (uint16_t)(code >> 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[(4 * piece + i) * 8] = (uint8_t)(code >> (8 * i));
+        }
+        if ((piece & 3) == 0) page[L::vs + ((tok >> 3) * (D / 32) + group) * 8 + (tok & 7)] = byte;
+    }
+}
+
+template <class E, int D, bool VEC>
+__global__ __launch_bounds__(256) void cache_read_kernel(const ReadArgs a) {
+    using L = PageLayout<D>;
+    constexpr int LPT = D / 4, HALF = LPT / 2;
+    const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LPT;
+    const int sub = threadIdx.x % LPT, piece = sub % HALF;
+    const bool is_v = sub >= HALF;
+    if (item >= (long long)a.T * a.H || (is_v ? !a.v : !a.k)) return;
+    const int t = (int)(item / a.H), h = (int)(item % a.H);
+    const int slot = a.slots[t];
+    f32x4 x0 = {0.f, 0.f, 0.f, 0.f}, x1 = x0;
+    if (slot >= 0 && slot / kPage < a.P) {
+        const uint8_t* page = a.store + ((long long)(slot / kPage) * a.H + h) * L::bytes;
+        const int tok = slot % kPage, group = piece >> 2;
+        const uint32_t kb = page[L::ks + k_scale_at<D>(tok, group)];
+        uint32_t code, byte = kb;
+        if (!is_v) {
+            code = *reinterpret_cast<const uint32_t*>(page + L::k + tok * (D / 2) + 4 * piece);
+        } else {
+            const uint8_t* from = page + L::v + ((tok >> 3) * 32 * 8 + (tok & 7)) * (D / 64);
+            if constexpr (D == 128) {
+                code = *reinterpret_cast<const uint16_t*>(from + (2 * piece) * 16) |
+                       ((uint32_t)*reinterpret_cast<const uint16_t*>(from + (2 * piece + 1) * 16) << 16);
+            } else {
+                code = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) code |= (uint32_t)from[(4 * piece + i) * 8] << (8 * i);
+            }
+            byte = page[L::vs + ((tok >> 3) * (D / 32) + group) * 8 + (tok & 7)];
+        }
+        const float scale = __uint_as_float(byte << 23);
+        const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 0), a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 1);
+        const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 2), a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 3);
+        x0 = f32x4{a0[0], a0[1], a1[0], a1[1]};
+        x1 = f32x4{a2[0], a2[1], a3[0], a3[1]};
+        if (kb == 255) {
+            const float nan = __uint_as_float(0x7fc00000u);
+            x0 = x1 = f32x4{nan, nan, nan, nan};
+        }
+    }
+    const Strides& st = is_v ? a.sv : a.sk;
+    void* dst = is_v ? a.v : a.k;
+    const long long at = h * st.h + t * st.n + 8 * piece;
+    store4<E, VEC>(dst, at, x0);
+    store4<E, VEC>(dst, at + 4, x1);
+}
+
+bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool aligned(const Strides& s, int size) { return ((s.b | s.h | s.n) * size & 15) == 0; }
+
+}  // namespace
+
+hipError_t launch_qk_norm_rope(const RopeArgs& a, hipStream_t st) {
+    const int size = a.dtype == 0 ? 2 : 4;
+    bool vec = aligned(a.wq) && aligned(a.wk) && aligned(a.cos) && aligned(a.sin);
+    if (a.Hq) vec = vec && aligned(a.q) && aligned(a.qo) && aligned(a.sq, size) && aligned(a.sqo, size);
+    if (a.Hk) vec = vec && aligned(a.k) && aligned(a.ko) && aligned(a.sk, size) && aligned(a.sko, size);
+    const long long tokens = (long long)a.B * a.N;
+    const int rows = 2048 / a.d;   // of a workgroup
+    const long long blocks = (tokens + rows - 1) / rows;
+    const int all = a.Hq + a.Hk;
+    const int heads = (int)std::min<long long>(std::max<long long>(blocks * all / 2048, 1), std::min(all, 16));
+    const dim3 grid((unsigned)blocks, (unsigned)((all + heads - 1) / heads));
+#define SOL_ROPE(E, D)                                                     \
+    do {                                                                   \
+        if (vec) qk_norm_rope_kernel<E, D, true><<<grid, 256, 0, st>>>(a, heads);   \
+        else qk_norm_rope_kernel<E, D, false><<<grid, 256, 0, st>>>(a, heads);      \
+    } while (0)
+    if (a.dtype == 0) {
+        if (a.d == 128) SOL_ROPE(BF16, 128);
+        else SOL_ROPE(BF16, 64);
+    } else {
+        if (a.d == 128) SOL_ROPE(F32, 128);
+        else SOL_ROPE(F32, 64);
+    }
+#undef SOL_ROPE
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_tables(const TablesArgs& a, hipStream_t st) {
+    const int grid = std::max(1, (int)(((long long)a.rows + kTablesRows - 1) / kTablesRows));
+    cache_tables_kernel<<<grid, kTablesThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st) {
+    const int size = a.dtype == 0 ? 2 : 4;
+    const bool vec = aligned(a.k) && aligned(a.v) && aligned(a.sk, size) && aligned(a.sv, size);
+    const unsigned grid = (unsigned)(((long long)a.T * a.H * (a.d / 4) + 255) / 256);
+#define SOL_APPEND(E, D)                                               \
+    do {                                                               \
+        if (vec) cache_append_kernel<E, D, true><<<grid, 256, 0, st>>>(a);      \
+        else cache_append_kernel<E, D, false><<<grid, 256, 0, st>>>(a);         \
+    } while (0)
+    if (a.dtype == 0) {
+        if (a.d == 128) SOL_APPEND(BF16, 128);
+        else SOL_APPEND(BF16, 64);
+    } else {
+        if (a.d == 128) SOL_APPEND(F32, 128);
+        else SOL_APPEND(F32, 64);
+    }
+#undef SOL_APPEND
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const ReadArgs& a, hipStream_t st) {
+    const int size = a.dtype == 0 ? 2 : 4;
+    const bool vec = aligned(a.k) && aligned(a.v) && (!a.k || aligned(a.sk, size)) && (!a.v || aligned(a.sv, size));
+    const unsigned grid = (unsigned)(((long long)a.T * a.H * (a.d / 4) + 255) / 256);
+#define SOL_READ(E, D)                                                 \
+    do {                                                               \
+        if (vec) cache_read_kernel<E, D, true><<<grid, 256, 0, st>>>(a);        \
+        else cache_read_kernel<E, D, false><<<grid, 256, 0, st>>>(a);           \
+    } while (0)
+    if (a.dtype == 0) {
+        if (a.d == 128) SOL_READ(BF16, 128);
+        else SOL_READ(BF16, 64);
+    } else {
+        if (a.d == 128) SOL_READ(F32, 128);
+        else SOL_READ(F32, 64);
+    }
+#undef SOL_READ
+    return hipGetLastError();
+}
+
+}  // namespace sol

@@ -1,0 +1,217 @@
+"""Host-side checks of the serving operators: exported symbols, refusals before any GPU call, the reference itself."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import sol_cache_oracle as ora
+from paper_2607_24027_amd import binding as sb
+from paper_2607_24027_amd import cache as sc
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "sol_cache.h")
+P = ctypes.c_void_p
+A, B_, C, D_, E, F, G, H, I, J = (P(0x100000 * (i + 1)) for i in range(10))   # never dereferenced
+INVALID, UNSUPPORTED, WORKSPACE = sb.SOL_ERR_INVALID_ARG, sb.SOL_ERR_UNSUPPORTED, sb.SOL_ERR_WORKSPACE
+
+
+def strides(*s):
+    return ctypes.cast((ctypes.c_longlong * len(s))(*s), P)
+
+
+def test_library_exports_every_declared_symbol():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(sol_\w+)\s*\(", text))
+    assert names == set(sc.SIGNATURES)
+    for name in names:
+        assert hasattr(sc.lib(), name), name
+    assert re.search(r"SOL_CACHE_PAGE = 64\b", text) and sc.PAGE == 64
+    assert re.search(r"SOL_ROPE_HALVES = 0, SOL_ROPE_PAIRS = 1\b", text) and (sc.HALVES, sc.PAIRS) == (0, 1)
+
+
+def rope(**kw):
+    a = dict(q=A, k=B_, qo=C, ko=D_, sq=strides(1, 1, 1), sk=strides(1, 1, 1), sqo=strides(1, 1, 1), sko=strides(1, 1, 1), wq=None,
+             wk=None, cos=E, sin=F, pos=G, B=1, Hq=4, Hk=2, N=10, d=128, P=100, rot=128, pairs=0, eps=1e-6, dtype=0, wdtype=0)
+    a.update(kw)
+    return sc.lib().sol_qk_norm_rope(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=None), INVALID), (dict(ko=None), INVALID), (dict(Hk=0), INVALID), (dict(qo=A), INVALID), (dict(qo=B_), INVALID),
+    (dict(ko=A), INVALID), (dict(ko=C), INVALID), (dict(sq=None), INVALID), (dict(sko=strides(1, -1, 1)), INVALID), (dict(B=0), INVALID),
+    (dict(N=-1), INVALID), (dict(d=96), UNSUPPORTED), (dict(dtype=2), INVALID), (dict(wdtype=3), INVALID), (dict(rot=12), INVALID),
+    (dict(rot=136), INVALID), (dict(rot=-8), INVALID), (dict(cos=None), INVALID), (dict(P=0), INVALID), (dict(pairs=2), INVALID),
+    (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID), (dict(pos=None, P=9), INVALID),
+    (dict(q=None, k=None, qo=None, ko=None, Hq=0, Hk=0), INVALID), (dict(Hq=65535), UNSUPPORTED),
+])
+def test_rope_refusals(kw, code):
+    assert rope(**kw) == code
+    assert sb.last_error()
+
+
+def tables(**kw):
+    a = dict(lens=A, add=B_, table=C, ring=D_, state=E, lens_out=F, state_out=G, row_start=H, slots=I, positions=J, S=4, MP=8, P=16,
+             rows=5)
+    a.update(kw)
+    return sc.lib().sol_cache_tables(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [(dict([(n, None)]), INVALID) for n in ("lens", "add", "table", "ring", "state", "lens_out",
+                                                                          "state_out", "row_start", "slots", "positions")] + [
+    (dict(S=0), INVALID), (dict(MP=0), INVALID), (dict(P=0), INVALID), (dict(rows=-1), INVALID), (dict(lens_out=A), INVALID),
+    (dict(state_out=E), INVALID), (dict(S=4097), UNSUPPORTED), (dict(P=(1 << 24) + 1), UNSUPPORTED),
+    (dict(S=4096, MP=1 << 20), UNSUPPORTED), (dict(rows=(1 << 30) + 1), UNSUPPORTED)])
+def test_tables_refusals(kw, code):
+    assert tables(**kw) == code
+    assert sb.last_error()
+
+
+def append(**kw):
+    a = dict(k=A, v=B_, sk=strides(1, 1), sv=strides(1, 1), store=C, slots=D_, T=4, H=2, d=128, P=4, dtype=0)
+    a.update(kw)
+    return sc.lib().sol_cache_append(*a.values(), None)
+
+
+def read(**kw):
+    a = dict(store=C, slots=D_, k=A, v=B_, sk=strides(1, 1), sv=strides(1, 1), T=4, H=2, d=128, P=4, dtype=0)
+    a.update(kw)
+    return sc.lib().sol_cache_read(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(k=None), INVALID), (dict(slots=None), INVALID), (dict(store=None), INVALID), (dict(store=P(0x300008)), INVALID),
+    (dict(T=0), INVALID), (dict(H=0), INVALID), (dict(P=0), INVALID), (dict(P=1 << 25), UNSUPPORTED), (dict(d=32), UNSUPPORTED),
+    (dict(dtype=7), INVALID), (dict(sk=None), INVALID), (dict(sv=strides(1, -2)), INVALID)])
+def test_append_and_read_refusals(kw, code):
+    assert append(**kw) == code
+    if kw == dict(k=None):
+        kw = dict(k=None, v=None)
+    assert read(**kw) == code
+    assert sb.last_error()
+
+
+def attn(**kw):
+    a = dict(q=A, sq=strides(1, 1), out=B_, so=strides(1, 1), store=C, table=D_, lens=E, row_start=F, positions=G, S=2, T=8, rows=4,
+             Hq=8, Hk=2, d=128, P=100, MP=50, G=1, dtype=0, ws=H, ws_bytes=1 << 40)
+    a.update(kw)
+    return sc.lib().sol_cache_forward(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [(dict([(n, None)]), INVALID) for n in ("q", "out", "store", "table", "lens", "row_start",
+                                                                          "positions", "sq", "so")] + [
+    (dict(out=A), INVALID), (dict(store=P(0x300004)), INVALID), (dict(S=0), INVALID), (dict(T=0), INVALID), (dict(rows=0), INVALID),
+    (dict(Hq=7), INVALID), (dict(Hk=0), INVALID), (dict(d=80), UNSUPPORTED), (dict(P=0), INVALID), (dict(MP=0), INVALID),
+    (dict(G=0), INVALID), (dict(dtype=4), INVALID), (dict(S=4097), UNSUPPORTED), (dict(T=1 << 28), UNSUPPORTED),
+    (dict(ws=None), WORKSPACE), (dict(ws_bytes=1000), WORKSPACE), (dict(ws=P(0x800004)), INVALID)])
+def test_forward_refusals(kw, code):
+    assert attn(**kw) == code
+    assert sb.last_error()
+
+
+def test_sizes():
+    assert sc.cache_bytes(10, 3, 128) == 10 * 3 * 68 * 128
+    for bad in ((0, 1, 64), (1, 0, 64), (1, 1, 96), (1 << 25, 1, 64)):
+        with pytest.raises(ValueError):
+            sc.cache_bytes(*bad)
+    assert sc.workspace_bytes(4, 4, 1, 8, 2, 128, 1000) > 0
+    with pytest.raises(ValueError):
+        sc.workspace_bytes(4, 4, 1, 8, 3, 128, 1000)
+
+
+def test_tensors_are_checked():
+    q, k = torch.zeros(1, 4, 6, 64), torch.zeros(1, 2, 6, 64)
+    with pytest.raises(ValueError, match="GPU"):
+        sc.qk_norm_rope(q, k)
+    with pytest.raises(ValueError, match="agree"):
+        sc.qk_norm_rope(q, torch.zeros(1, 2, 5, 64))
+    with pytest.raises(ValueError, match="contiguous"):
+        sc.qk_norm_rope(q.transpose(2, 3), None)
+    with pytest.raises(ValueError, match="dtype"):
+        sc.qk_norm_rope(q, k.bfloat16())
+    with pytest.raises(TypeError):
+        sc.qk_norm_rope(q.half(), None)
+    with pytest.raises(ValueError, match="overlap"):
+        sc.qk_norm_rope(q, None, q_out=q)
+    with pytest.raises(ValueError, match="rows of q_out overlap"):
+        sc.qk_norm_rope(q, None, q_out=torch.zeros(64).expand(1, 4, 6, 64))
+    with pytest.raises(ValueError, match="together"):
+        sc.qk_norm_rope(q, k, cos=torch.zeros(6, 32))
+    with pytest.raises(ValueError, match="positions"):
+        sc.qk_norm_rope(q, k, cos=torch.zeros(6, 32), sin=torch.zeros(6, 32), positions=torch.zeros(6, dtype=torch.int32))
+    i32 = dict(dtype=torch.int32)
+    lens, add, table, ring, state = torch.zeros(3, **i32), torch.zeros(3, **i32), torch.zeros(3, 4, **i32), torch.zeros(9, **i32), torch.zeros(2, **i32)
+    with pytest.raises(ValueError, match="GPU"):
+        sc.tables(lens, add, table, ring, state, 5)
+    with pytest.raises(ValueError, match="add"):
+        sc.tables(lens, add[:2], table, ring, state, 5)
+    with pytest.raises(ValueError, match="dtype"):
+        sc.tables(lens.long(), add, table, ring, state, 5)
+    step = sc.Step(torch.zeros(4, **i32), torch.zeros(5, **i32), torch.zeros(5, **i32), lens, torch.zeros(2, **i32))
+    with pytest.raises(ValueError, match="overlap"):
+        sc.tables(lens, add, table, ring, state, 5, out=step)
+    store = torch.zeros(5, 2, 68 * 64, dtype=torch.uint8)
+    k = torch.zeros(2, 7, 64)
+    slots = torch.zeros(7, **i32)
+    with pytest.raises(ValueError, match="GPU"):
+        sc.append(k, k, store, slots)
+    with pytest.raises(ValueError, match="heads"):
+        sc.append(k[:1], k[:1], store, slots)
+    with pytest.raises(ValueError, match="slots"):
+        sc.append(k, k, store, slots[:3])
+    with pytest.raises(ValueError, match="store"):
+        sc.append(k, k, store[:, :, :100], slots)
+    with pytest.raises(TypeError):
+        sc.read(store, slots, dtype=torch.float16)
+    args = (store, table, lens, torch.zeros(4, **i32), torch.zeros(7, **i32))
+    q = torch.zeros(4, 7, 64)
+    with pytest.raises(ValueError, match="GPU"):
+        sc.forward(q, *args)
+    with pytest.raises(ValueError, match="channels"):
+        sc.forward(torch.zeros(4, 7, 128), *args)
+    with pytest.raises(ValueError, match="overlap"):
+        sc.forward(q, *args, out=q)
+    with pytest.raises(ValueError, match="positions"):
+        sc.forward(torch.zeros(4, 8, 64), *args)
+
+
+def test_reference_quantiser():
+    x = np.zeros((1, 32))
+    x[0, :10] = [6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 0.2501, -0.25]
+    code, e = ora.quantise(x, ora.K_SCALES)
+    assert e.tolist() == [[0]]
+    assert code[0, :10].tolist() == [7, 0, 2, 2, 4, 4, 6, 6, 1, 8]      # ties to the even code
+    for top, want in ((7.0, 0), (7.0001, 1), (8.0, 1), (3.99, 0), (3.5, -1), (3.5001, 0), (4.0, 0)):
+        assert ora.quantise(np.full((1, 32), top), ora.K_SCALES)[1].tolist() == [[want]], top
+    assert ora.quantise(np.full((1, 32), 1e30), ora.V_SCALES)[1].tolist() == [[13]]
+    assert ora.quantise(np.full((1, 32), 1e-30), ora.V_SCALES)[1].tolist() == [[-23]]
+    assert ora.quantise(np.zeros((1, 32)), ora.K_SCALES)[1].tolist() == [[-100]]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_reference_pages_keep_what_is_written(d):
+    rng = np.random.default_rng(d)
+    page = np.zeros(68 * d, np.uint8)
+    kv = rng.standard_normal((2, 64, d)) * 3
+    (kc, ke), (vc, ve) = ora.quantise(kv[0], ora.K_SCALES), ora.quantise(kv[1], ora.V_SCALES)
+    for t in rng.permutation(64):
+        ora.write_page_token(page, t, d, (kc[t], ke[t]), (vc[t], ve[t]))
+    k, v = ora.read_page(page, d)
+    assert np.array_equal(k, ora.values(kc, ke)) and np.array_equal(v, ora.values(vc, ve))
+
+
+def test_reference_tables_by_hand():
+    # two requests: 60 tokens on page 3, 64 tokens on page 1; free pages 5, 0 in front
+    table = np.array([[3, -1], [1, -1]])
+    ring = np.array([5, 0, -1, -1, -1, -1])
+    got = ora.tables([60, 64], [6, 1], table, ring, [0, 2], 9)
+    assert got[0].tolist() == [0, 6, 7]
+    assert got[1].tolist() == [252, 253, 254, 255, 320, 321, 0, -1, -1]
+    assert got[2].tolist() == [60, 61, 62, 63, 64, 65, 64, -1, -1]
+    assert got[3].tolist() == [66, 65] and got[4].tolist() == [2, 0]
+    assert got[5].tolist() == [[3, 5], [1, 0]]
+    got = ora.tables(got[3], [-7, 64], got[5], got[6], got[4], 64)      # the first gives page 5 back, the second is refused
+    assert got[3].tolist() == [59, 65] and got[4].tolist() == [2, 1] and got[6][2] == 5
+    assert (got[1] == -1).all() and (got[2] == -1).all()

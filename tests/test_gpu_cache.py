@@ -1,0 +1,621 @@
+"""GPU parity of the serving operators against the 64-bit reference (oracle/sol_cache_oracle.py).
+
+Tolerances count roundings.  A bf16 value is off by at most 2^-8 of itself, an f32 value by 2^-24.  The other terms are
+stated at each check.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import sol_cache_oracle as ora
+from paper_2607_24027_amd import binding as sb
+from paper_2607_24027_amd import cache as sc
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    sc.lib()
+    return torch.device("cuda:0")
+
+
+def i32(x, dev):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=dev)
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def placed(x, how, dev):
+    """x [..., d] on the GPU as a view of that kind: 'plain', 'tokens' (the last two leading dimensions exchanged in memory),
+    'odd' (rows that start anywhere)."""
+    x = x.to(dev)
+    if how == "tokens":
+        return x.transpose(-3, -2).contiguous().transpose(-3, -2)
+    if how == "odd":
+        big = torch.zeros(*x.shape[:-1], x.shape[-1] + 3, dtype=x.dtype, device=dev)
+        big[..., 1:-2] = x
+        return big[..., 1:-2]
+    return x.contiguous()
+
+
+# ------------------------------------------------------------------------------------------------ norm and rotation
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rot,pairs,how,B,N,Hq,Hk", [
+    (128, 128, False, "plain", 1, 1, 1, 1), (128, 128, True, "tokens", 2, 37, 5, 3), (128, 0, False, "tokens", 1, 16, 2, 2),
+    (128, 64, False, "odd", 1, 19, 3, 1), (128, 24, True, "plain", 1, 33, 2, 7), (128, 8, False, "tokens", 3, 5, 4, 0),
+    (64, 64, False, "tokens", 1, 70, 9, 2), (64, 64, True, "odd", 1, 8, 2, 2), (64, 32, False, "plain", 2, 129, 1, 4),
+    (64, 40, True, "tokens", 1, 65, 0, 3), (128, 128, False, "tokens", 1, 700, 40, 8),
+])
+def test_qk_norm_rope(dev, dtype, d, rot, pairs, how, B, N, Hq, Hk):
+    g = torch.Generator().manual_seed(d + rot + N)
+    P = 50
+    xs = [torch.randn(B, H, N, d, generator=g).mul(torch.exp2(torch.randint(-6, 7, (B, H, N, 1), generator=g))).to(DT[dtype])
+          if H else None for H in (Hq, Hk)]
+    for x in xs:
+        if x is not None:
+            x[0, 0, 0] = 0.0                                     # a row without a length
+    ws = [torch.randn(d, generator=g).to(DT[dtype]) if x is not None else None for x in xs]
+    if how == "plain":
+        ws[1] = None
+    cos = sin = None
+    if rot:
+        angle = torch.rand(P, rot // 2, generator=g, dtype=torch.float64) * 7
+        cos, sin = angle.cos().float(), angle.sin().float()
+    positions = torch.randint(0, P, (B, N), generator=g, dtype=torch.int32)
+    positions[torch.rand(B, N, generator=g) < 0.2] = -1
+    positions[-1, -1] = P if rot else -5                         # not a row of the tables
+    gpu = [None if x is None else placed(x, how, dev) for x in xs]
+    outs = [None if x is None else placed(torch.full(x.shape, 7.0, dtype=x.dtype), how, dev) for x in xs]
+    got = sc.qk_norm_rope(gpu[0], gpu[1], *(None if w is None else w.to(dev) for w in ws), None if cos is None else cos.to(dev),
+                          None if sin is None else sin.to(dev), positions.to(dev), eps=1e-5, interleaved=pairs, q_out=outs[0],
+                          k_out=outs[1])
+    for x, w, y in zip(xs, ws, got):
+        if x is None:
+            assert y is None
+            continue
+        ref, written = ora.norm_rope(f64(x), None if w is None else f64(w), None if cos is None else cos.numpy(),
+                                     None if sin is None else sin.numpy(), positions.numpy(), 1e-5, pairs)
+        y = f64(y)
+        mask = np.broadcast_to(written[:, None, :, None], y.shape)
+        assert (y[~mask] == 7.0).all()
+        # f32: the sum of squares is off by at most 8 + 6 roundings, half of that in its root, then root, quotient, two factors
+        # (2 + 3 + 2) and two products and a sum of the pair: below 24 roundings of the pair's length.
+        length = np.abs(ref)
+        half = rot // 2
+        if half:
+            ia = np.arange(half) * 2 if pairs else np.arange(half)
+            ib = ia + 1 if pairs else ia + half
+            length[..., ia] = length[..., ib] = np.hypot(ref[..., ia], ref[..., ib])
+        tol = HALF_STEP[dtype] * np.abs(ref) * (1 + 2.0 ** -7) + 24 * 2.0 ** -24 * length
+        assert (np.abs(y - ref)[mask] <= tol[mask]).all()
+
+
+def test_qk_norm_rope_far_strides_and_defaults(dev):
+    # offsets past 2^31 elements in a strided view; default outputs and positions
+    big = torch.zeros(1, 3, 1 << 23, 128, dtype=torch.bfloat16, device=dev)      # 6.4 GB
+    g = torch.Generator().manual_seed(3)
+    part = torch.randn(1, 3, 5, 128, generator=g).bfloat16()
+    q = big[:, :, -5:]
+    q.copy_(part.to(dev))
+    angle = torch.rand(5, 64, generator=g, dtype=torch.float64)
+    y, none = sc.qk_norm_rope(q, None, cos=angle.cos().float().to(dev), sin=angle.sin().float().to(dev))
+    assert none is None and y.is_contiguous()
+    ref, _ = ora.norm_rope(f64(part), None, angle.cos().float().numpy(), angle.sin().float().numpy(), np.arange(5)[None], 1e-6, False)
+    assert (np.abs(f64(y) - ref) <= 2.0 ** -8 * np.abs(ref) * 1.01 + 2.0 ** -18).all()
+
+
+# ------------------------------------------------------------------------------------------------------ page tables
+def run_tables(dev, lens, add, table, ring, state, rows):
+    t, r = i32(table, dev), i32(ring, dev)
+    new = sc.tables(i32(lens, dev), i32(add, dev), t, r, i32(state, dev), rows)
+    return [x.cpu().numpy() for x in (new.row_start, new.slots, new.positions, new.lens, new.state, t, r)]
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_tables_random_steps(dev, seed):
+    rng = np.random.default_rng(seed)
+    S = int(rng.choice([1, 2, 63, 64, 65, 300, 1025, 4096]) if seed < 16 else rng.integers(1, 40))
+    MP = int(rng.integers(1, 30))
+    lens = rng.integers(0, MP * 64 + 1, S)
+    if seed % 3 == 0:
+        lens[rng.random(S) < 0.5] //= 64
+        lens[rng.random(S) < 0.3] = 0
+    held = -(-lens // 64)
+    P = int(held.sum() + rng.integers(1, 2 * S + 5))
+    pages = rng.permutation(P)
+    table = np.full((S, MP), -1)
+    table[np.arange(MP)[None] < held[:, None]] = pages[:held.sum()]
+    head = int(rng.integers(0, P))
+    ring = np.full(P, -1)
+    free = P - held.sum()
+    ring[(head + np.arange(free)) % P] = pages[held.sum():]
+    state = np.array([head, free])
+    table[rng.random(table.shape) < 0.02] = -1                   # pages that were dropped
+    for step in range(3):
+        add = rng.integers(-100, 150, S)
+        add[rng.random(S) < 0.2] = 0
+        add[rng.random(S) < 0.1] = -(1 << 30)
+        add[rng.random(S) < 0.02] = 1 << 30 if step == 2 else 64 * 31
+        rows = min(int(np.maximum(add, 0).astype(np.int64).sum()), 300000) + int(rng.integers(0, 50))
+        got = run_tables(dev, lens, add, table, ring, state, rows)
+        if np.maximum(add, 0).sum() > 300000:                    # the plain form goes row by row
+            add = np.minimum(add, 64 * 31)
+            got = run_tables(dev, lens, add, table, ring, state, rows)
+        want = ora.tables(lens, add, table, ring, state, rows)
+        for name, x, y in zip(("row_start", "slots", "positions", "lens", "state", "table", "ring"), got, want):
+            assert np.array_equal(x, y), (name, step)
+        lens, state, table, ring = want[3], want[4], want[5], want[6]
+
+
+def test_tables_more_rows_than_an_int_counts(dev):
+    # refused requests keep their rows: the sums stop at the largest int
+    add = [1 << 30] * 5 + [3]
+    got = run_tables(dev, [0] * 6, add, np.full((6, 2), -1), np.arange(4), [0, 4], 10)
+    assert got[0].tolist() == [0, 1 << 30] + [(1 << 31) - 1] * 5
+    assert (got[1] == -1).all() and got[3].tolist() == [0] * 5 + [3] and got[5][5, 0] == 0
+
+
+def test_tables_bad_values_stay_in_bounds(dev):
+    got = run_tables(dev, [-5, 1 << 30, 100], [70, -3, 5], [[9, 99], [7, -7], [1 << 30, 2]], [3, 1 << 30, -9, 2], [-3, 1 << 30], 80)
+    want = ora.tables([-5, 1 << 30, 100], [70, -3, 5], np.array([[9, 99], [7, -7], [1 << 30, 2]]), np.array([3, 1 << 30, -9, 2]),
+                      [-3, 1 << 30], 80)
+    for x, y in zip(got, want):
+        assert np.array_equal(x, y)
+
+
+def test_tables_give_the_same_step_again(dev):
+    lens, add = i32([100, 64, 0], dev), i32([40, -64, 10], dev)
+    table, ring, state = i32([[0, 1, -1], [2, -1, -1], [-1, -1, -1]], dev), i32([3, 4, 5, -1, -1, -1], dev), i32([0, 3], dev)
+    a = sc.tables(lens, add, table, ring, state, 50)
+    keep = [x.clone() for x in (*a, table, ring)]
+    b = sc.tables(lens, add, table, ring, state, 50, out=a)
+    assert b is a and all(torch.equal(x, y) for x, y in zip((*b, table, ring), keep))
+    last = sc.tables(lens, -lens, table, ring, state, 0)         # no rows at all
+    assert last.slots.numel() == 0 and last.lens.tolist() == [0, 0, 0]
+
+
+# -------------------------------------------------------------------------------------------------- append and read
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,H,T,how", [(128, 1, 1, "plain"), (128, 3, 200, "tokens"), (128, 8, 48, "odd"), (64, 1, 1, "odd"), (64, 5, 131, "tokens"),
+                                       (64, 2, 64, "plain")])
+def test_append_and_read(dev, dtype, d, H, T, how):
+    rng = np.random.default_rng(d + T)
+    P = -(-T // 64) + 2
+    k = rng.standard_normal((H, T, d)) * np.exp2(rng.integers(-12, 12, (H, T, 1)))
+    v = rng.standard_normal((H, T, d)) * np.exp2(rng.integers(-12, 12, (H, T, 1)))
+    k[0, 0, :32] = 0.0
+    v[-1, -1, :32] = np.resize([6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, -0.25, -5], 32)        # ties
+    k[0, -1, -32:] = 7.0
+    k, v = (torch.tensor(x).to(DT[dtype]) for x in (k, v))
+    if T > 8:
+        k[0, 3, :32], v[0, 3, :32] = 3e38, 1e5                   # past what a value's scale may be
+        k[0, 4, :32], v[0, 4, :32] = 1e-38, 1e-38
+        k[0, 5, 1], v[0, 6, 2] = 2e-20, 2.0 ** -25
+    slots = rng.permutation(P * 64)[:T].astype(np.int32)
+    if how == "tokens":
+        slots = (np.arange(T) + 37).astype(np.int32)
+    skip = rng.random(T) < 0.1
+    skip[0] = False
+    slots[skip] = rng.choice([-1, -(1 << 31), P * 64, (1 << 31) - 1], skip.sum())
+    before = torch.randint(0, 256, (P, H, 68 * d), dtype=torch.uint8, generator=torch.Generator().manual_seed(1))
+    store = before.to(dev)
+    sc.append(placed(k, how, dev), placed(v, how, dev), store, i32(slots, dev))
+    want = before.numpy().copy()
+    (kc, ke), (vc, ve) = ora.quantise(f64(k), ora.K_SCALES), ora.quantise(f64(v), ora.V_SCALES)
+    for t in range(T):
+        if not skip[t]:
+            for h in range(H):
+                ora.write_page_token(want[slots[t] // 64, h], int(slots[t] % 64), d, (kc[h, t], ke[h, t]), (vc[h, t], ve[h, t]))
+    assert np.array_equal(store.cpu().numpy(), want)             # every byte, those of other tokens too
+    rk, rv = ora.values(kc, ke), ora.values(vc, ve)
+    rk[:, skip] = rv[:, skip] = 0.0
+    for dt in ("bf16", "f32"):
+        gk, gv = sc.read(store, i32(slots, dev), dtype=DT[dt])
+        assert np.array_equal(f64(gk), rk) and np.array_equal(f64(gv), rv)
+    out = placed(torch.full((H, T, d), 5.0), how, dev)
+    nothing, only = sc.read(store, i32(slots, dev), v_out=out)
+    assert nothing is None and only is out and np.array_equal(f64(out), rv)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_tokens_that_are_not_finite(dev, d):
+    k, v = torch.randn(2, 6, d), torch.randn(2, 6, d)
+    k[0, 1, 5], v[1, 2, d - 1], k[1, 3, 0], v[0, 4, 40] = math.nan, math.inf, -math.inf, math.nan
+    store = sc.empty(1, 2, d, dev)
+    slots = i32([9, 63, 0, 17, 40, 41], dev)
+    sc.append(k.to(dev), v.to(dev), store, slots)
+    gk, gv = (f64(x) for x in sc.read(store, slots, dtype=torch.float32))
+    bad = np.zeros((2, 6), bool)
+    bad[0, 1] = bad[1, 2] = bad[1, 3] = bad[0, 4] = True
+    assert np.isnan(gk[bad]).all() and np.isnan(gv[bad]).all()
+    assert np.isfinite(gk[~bad]).all() and np.isfinite(gv[~bad]).all()
+
+
+# ----------------------------------------------------------------------------------------------------- attention
+def make_store(rng, P, H, d, dev, fill=None):
+    """A store whose tokens were appended, and its values [H, P * 64, d]."""
+    k = torch.tensor(rng.standard_normal((H, P * 64, d)) * np.exp(0.4 * rng.standard_normal((H, 1, d))), dtype=torch.float32)
+    v = torch.tensor(rng.standard_normal((H, P * 64, d)) + 0.5 * rng.standard_normal((H, 1, d)), dtype=torch.float32)
+    store = sc.empty(P, H, d, dev)
+    if fill is not None:
+        store.fill_(fill)
+    slots = torch.arange(P * 64, dtype=torch.int32, device=dev)
+    sc.append(k.to(dev), v.to(dev), store, slots)
+    return store, ora.values(*ora.quantise(k.numpy().astype(np.float64), ora.K_SCALES)), \
+        ora.values(*ora.quantise(v.numpy().astype(np.float64), ora.V_SCALES))
+
+
+def tolerance(dtype, q, k, out, spread, reach):
+    """Bound of the error of one row of outputs.  With ds the error of a logit, a probability is off by 2 ds of itself at most
+    (ds is small), and an output by that times sum p |v - out|: weights that all change alike leave it as it is.
+
+    ds: the terms that q is split into leave 2^-13 of the largest of 32 channels where a channel is below 1/60 of that (bf16), or
+    2^-24 of it (f32); sums of d products in f32, 2^-24 a term, on sum |q k|; the argument of the exponential, 4 roundings
+    of a number below |s| + 16.  Probabilities are cut to f16: 2^-10 (bf16), or in two terms 2^-20 (f32), and below 2^-21 of the
+    largest to steps of 2^-31 of it.  Sums of probabilities times values: f32, at most one rounding for 16 keys and 64 more for
+    shares and their join, on sum p |v|.  The result: one rounding of its type, and a quotient."""
+    d, L = q.shape[0], k.shape[0]
+    block = np.abs(q).reshape(-1, 32)
+    top = np.repeat(block.max(1), 32)
+    lost = np.where(np.abs(q) <= top / 60, top * 2.0 ** -13, 0.0) if dtype == "bf16" else top * 2.0 ** -24
+    s = np.abs(k) @ np.abs(q) / math.sqrt(d)
+    ds = (np.abs(k) @ lost) / math.sqrt(d) + d * 2.0 ** -24 * s + 4 * 2.0 ** -24 * (s + 16)
+    cut = 2.0 ** -10 if dtype == "bf16" else 2.0 ** -20
+    return (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * np.abs(out) + (2 * ds.max() + cut) * spread + L * 2.0 ** -31 * (spread + np.abs(out)) \
+        + (L / 16 + 64) * 2.0 ** -24 * reach
+
+
+def check_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how="tokens", seed=0, positions=None, drop=(), max_rows=None, extra=0,
+                  fill=255, atol_rows=None):
+    """One call against the reference; lens: with the new rows."""
+    rng = np.random.default_rng(seed)
+    S = len(lens)
+    held = [-(-n // 64) for n in lens]
+    P = sum(held) + 2
+    store, k, v = make_store(rng, P, Hk, d, dev)
+    pages = rng.permutation(P)
+    MP = max(held + [1]) + 1
+    table = rng.integers(-1, 2 * P, (S, MP))                     # what lies behind a request's pages is never read
+    at = 0
+    raw = store.cpu().numpy()
+    for s in range(S):
+        table[s, :held[s]] = pages[at:at + held[s]]
+        at += held[s]
+    keep = np.zeros((P, 64), bool)
+    for s in range(S):
+        for t in range(lens[s]):
+            keep[table[s, t // 64], t % 64] = True
+    # bytes of tokens that are in no request are the worst there are
+    for p in range(P):
+        if not keep[p].any():
+            raw[p] = fill
+        elif not keep[p].all():
+            n = int(keep[p].sum())
+            for h in range(Hk):
+                for t in range(n, 64):
+                    w = d // 64
+                    raw[p, h, t * (d // 2):(t + 1) * (d // 2)] = fill
+                    t2 = (t & 0b10011) | (((t >> 2) & 1) << 3) | (((t >> 3) & 1) << 2)
+                    for g in range(d // 32):
+                        raw[p, h, 32 * d + (((g % 2) * 32 + t2 % 32) * w + g // 2) * 2 + t // 32] = fill
+                        raw[p, h, 66 * d + ((t // 8) * (d // 32) + g) * 8 + t % 8] = fill
+    store = torch.tensor(raw, device=dev)
+    for s, p, bad in drop:
+        table[s, p] = bad
+    T = sum(rows) + extra
+    q = torch.tensor(rng.standard_normal((Hq, T, d)), dtype=torch.float32).to(DT[dtype])
+    if positions is None:
+        positions = np.concatenate([np.arange(n - r, n) for n, r in zip(lens, rows)] + [np.full(extra, 3)]) if T else np.zeros(0)
+    row_start = np.concatenate([[0], np.cumsum(rows)])
+    out = placed(torch.full((Hq, T, d), 9.0, dtype=DT[dtype]), how, dev)
+    args = (placed(q, how, dev), store, i32(table, dev), i32(lens, dev), i32(row_start, dev), i32(positions, dev))
+    got = sc.forward(*args, causal_granule=granule, max_rows=max_rows, out=out)
+    assert got is out
+    y, qn = f64(out), f64(q)
+    assert (y[:, sum(rows):] == 9.0).all()
+    G = Hq // Hk
+    worst = 0.0
+    for s in range(S):
+        n = lens[s]
+        ok = np.array([0 <= table[s, t // 64] < P for t in range(n)], bool)
+        slots = np.array([table[s, t // 64] * 64 + t % 64 if ok[t] else 0 for t in range(n)], int)
+        r0, r1 = row_start[s], row_start[s + 1]
+        if max_rows is not None:
+            r1 = min(r1, r0 + max_rows)
+        if r1 == r0:
+            continue
+        pos = positions[r0:r1]
+        limit = np.where(pos < 0, 0, np.minimum((pos // granule + 1) * granule, n))
+        sees = (np.arange(n)[None] < limit[:, None]) & ok[None]
+        for h in range(Hq):
+            kk, vv = k[h // G][slots], v[h // G][slots]
+            ref, spread, reach = ora.attend(qn[h, r0:r1], kk, vv, sees)
+            for r in range(r1 - r0):
+                tol = tolerance(dtype, qn[h, r0 + r], kk if n else np.zeros((1, d)), ref[r], spread[r], reach[r])
+                err = np.abs(y[h, r0 + r] - ref[r])
+                assert (err <= tol).all(), (s, h, r, float((err / np.maximum(tol, 1e-300)).max()))
+                worst = max(worst, float((err / np.maximum(tol, 1e-300)).max()))
+    # the same call again gives the same bits
+    again = sc.forward(*args, causal_granule=granule, max_rows=max_rows, out=torch.full_like(out, 9.0))
+    assert torch.equal(again, out)
+    return worst
+
+
+FORWARD = [
+    # d, Hq, Hk, lens, rows, granule, layout
+    (128, 1, 1, [1], [1], 1, "plain"),
+    (128, 8, 2, [64], [1], 1, "tokens"),
+    (64, 6, 2, [65, 1, 300], [1, 1, 1], 1, "odd"),
+    (128, 4, 1, [1000], [1], 1, "tokens"),
+    (64, 3, 3, [700, 63, 128], [5, 63, 1], 1, "tokens"),
+    (128, 10, 2, [200, 77], [40, 77], 1, "plain"),
+    (128, 2, 2, [333], [150], 37, "odd"),
+    (64, 4, 4, [500], [260], 100, "tokens"),
+    (128, 3, 1, [400, 90], [200, 30], 1 << 30, "tokens"),
+    (64, 8, 1, [2000], [9], 1, "plain"),
+    (128, 33, 1, [130], [2], 1, "tokens"),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,Hq,Hk,lens,rows,granule,how", FORWARD)
+def test_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how):
+    check_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how, seed=d + sum(lens))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fill", [0, 127, 254, 255])
+def test_forward_empty_requests_and_rows(dev, dtype, fill):
+    # no tokens, no rows, rows that see nothing, rows behind the last request, whatever lies behind the lengths
+    positions = np.array([-1, 0, 5, 89, -1, 2, 3, 3])
+    check_forward(dev, dtype, 128, 4, 2, [90, 0, 70, 0, 4], [4, 2, 0, 0, 1], 1, positions=positions, extra=1, fill=fill, seed=fill)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 150])
+def test_forward_dropped_pages(dev, dtype, rows):
+    drop = [(0, 0, -1), (0, 3, 1 << 30), (0, 4, -(1 << 31)), (1, 0, -1), (1, 1, -1), (1, 2, -1)]
+    check_forward(dev, dtype, 64, 4, 2, [600, 160], [rows, 1], 1, drop=drop, seed=rows)
+
+
+@pytest.mark.parametrize("rows", [[3, 200], [1, 40]])
+def test_forward_max_rows_leaves_the_rest(dev, rows):
+    rng = np.random.default_rng(5)
+    store, _, _ = make_store(rng, 8, 1, 128, dev)
+    q = torch.randn(2, sum(rows), 128, device=dev)
+    args = (store, i32([[0, 1, 2, 3], [4, 5, 6, 7]], dev), i32([250, 256], dev), i32(np.cumsum([0] + rows), dev),
+            i32(list(range(rows[0])) + list(range(rows[1])), dev))
+    full = sc.forward(q, *args)
+    part = sc.forward(q, *args, max_rows=max(rows))
+    assert torch.equal(full, part)
+    workspace = torch.empty(sc.workspace_bytes(2, sum(rows), max(rows), 2, 1, 128, 4), dtype=torch.uint8, device=dev)
+    assert torch.equal(sc.forward(q, *args, max_rows=max(rows), workspace=workspace), full)
+    with pytest.raises(sb.SolAttnError):
+        sc.forward(q, *args, max_rows=max(rows), workspace=workspace[:16])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_forward_not_finite(dev, dtype):
+    """A token held as NaN, and queries that are not finite: their rows are NaN, every other row is as without them."""
+    rng = np.random.default_rng(8)
+    d, T = 128, 130
+    k, v = (torch.tensor(rng.standard_normal((1, 200, d)), dtype=torch.float32, device=dev) for _ in range(2))
+    q = torch.tensor(rng.standard_normal((2, T, d)), dtype=torch.float32, device=dev).to(DT[dtype])
+    table, lens, row_start = i32([[2, 0, 3, 1]], dev), i32([200], dev), i32([0, T], dev)
+    slots = i32([[2, 0, 3, 1][t // 64] * 64 + t % 64 for t in range(200)], dev)
+    positions = i32(np.arange(70, 200), dev)
+
+    def run(bad_k=None, bad_v=None, bad_q=None):
+        kk, vv, qq = k.clone(), v.clone(), q.clone()
+        if bad_k is not None:
+            kk[0, bad_k, 77] = math.nan
+        if bad_v is not None:
+            vv[0, bad_v, 3] = math.inf
+        if bad_q is not None:
+            qq[1, bad_q, 100] = math.inf
+        store = sc.empty(4, 1, d, dev)
+        store.fill_(255)
+        sc.append(kk, vv, store, slots)
+        return sc.forward(qq, store, table, lens, row_start, positions)
+    clean = run()
+    assert bool(torch.isfinite(clean).all())
+    for kw in (dict(bad_k=110), dict(bad_v=131), dict(bad_k=199)):
+        at = next(iter(kw.values()))
+        y = run(**kw)
+        sees = (positions >= at)[None, :, None].expand_as(y)
+        assert bool(torch.isnan(y[sees]).all()) and torch.equal(y[~sees], clean[~sees])
+    y = run(bad_q=17)
+    assert bool(torch.isnan(y[1, 17]).all())
+    y[1, 17] = clean[1, 17]
+    assert torch.equal(y, clean)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("peak", [0, 3000, 69999])
+def test_forward_long_and_peaked(dev, dtype, peak):
+    """70,000 tokens, of which one has nearly all the weight; a maximum that comes late."""
+    d, L = 128, 70000
+    P = -(-L // 64)
+    g = torch.Generator(device=dev).manual_seed(peak)
+    k, v = (torch.randn(1, P * 64, d, generator=g, device=dev) for _ in range(2))
+    q = torch.randn(1, 1, d, generator=g, device=dev).to(DT[dtype])
+    k[0, peak] = q.float()[0, 0] * 3
+    store = sc.empty(P, 1, d, dev)
+    order = torch.randperm(P, generator=g, device=dev)
+    slots = (order[:, None] * 64 + torch.arange(64, device=dev)).flatten().int()
+    sc.append(k, v, store, slots)
+    out = sc.forward(q, store, order[None].int(), i32([L], dev), i32([0, 1], dev), i32([L - 1], dev))
+    kk, vv = (f64(x)[0, :L] for x in sc.read(store, slots, dtype=torch.float32))
+    ref, spread, reach = ora.attend(f64(q)[0], kk, vv, np.ones((1, L), bool))
+    tol = tolerance(dtype, f64(q)[0, 0], kk, ref[0], spread[0], reach[0])
+    assert (np.abs(f64(out)[0, 0] - ref[0]) <= tol).all()
+
+
+def test_forward_many_requests(dev):
+    """More requests than lanes: 300 of them, some with several rows, some with none."""
+    rng = np.random.default_rng(11)
+    lens = [int(x) for x in rng.integers(0, 200, 300)]
+    rows = [min(n, int(r)) for n, r in zip(lens, rng.choice([0, 1, 1, 1, 2, 40], 300))]
+    check_forward(dev, "bf16", 64, 2, 1, lens, rows, 1, seed=12)
+
+
+# ------------------------------------------------------------------------------------------------------ as one step
+class Server:
+    """Requests that grow step by step through the four operators; the reference keeps plain lists."""
+
+    def __init__(self, dev, dtype, d, Hq, Hk, S, MP, P, seed, interleaved):
+        self.dev, self.dtype, self.d, self.Hq, self.Hk, self.S = dev, dtype, d, Hq, Hk, S
+        self.rng = np.random.default_rng(seed)
+        self.lens, self.state = i32([0] * S, dev), i32([0, P], dev)
+        self.table, self.ring = i32(np.full((S, MP), -1), dev), i32(self.rng.permutation(P), dev)
+        self.store = sc.empty(P, Hk, d, dev)
+        self.store.fill_(255)
+        angle = np.arange(MP * 64)[:, None] * 100.0 ** (-np.arange(d // 2) / (d // 2))
+        self.cos, self.sin = (torch.tensor(f(angle), dtype=torch.float32, device=dev) for f in (np.cos, np.sin))
+        self.w = [torch.tensor(1 + 0.1 * self.rng.standard_normal(d), dtype=torch.float32, device=dev) for _ in range(2)]
+        self.inter = interleaved
+        self.held = [[np.zeros((Hk, 0, d))] * 2 for _ in range(S)]
+
+    def qkv(self, rows):
+        x = self.rng.standard_normal((rows, self.Hq + 2 * self.Hk, self.d))
+        return torch.tensor(x, dtype=torch.float32, device=self.dev).to(DT[self.dtype])
+
+    def split(self, qkv):
+        x = qkv.transpose(0, 1)
+        return x[:self.Hq], x[self.Hq:self.Hq + self.Hk], x[self.Hq + self.Hk:]
+
+    def step(self, qkv, add, granule=1):
+        """The calls of one step on tensors `qkv` [rows, heads, d] and add [S]."""
+        q, k, v = self.split(qkv)
+        new = sc.tables(self.lens, add, self.table, self.ring, self.state, qkv.shape[0])
+        q, k = sc.qk_norm_rope(q[None], k[None], *self.w, self.cos, self.sin, new.positions[None], interleaved=self.inter)
+        sc.append(k[0], v, self.store, new.slots)
+        out = sc.forward(q[0], self.store, self.table, new.lens, new.row_start, new.positions, causal_granule=granule)
+        return new, q[0], k[0], out
+
+    def check(self, qkv, add, new, q, k, out, granule=1):
+        _, _, v = self.split(qkv)
+        kq = ora.values(*ora.quantise(f64(k), ora.K_SCALES))
+        vq = ora.values(*ora.quantise(f64(v), ora.V_SCALES))
+        at = 0
+        for s, a in enumerate(add):
+            ks, vs = self.held[s]
+            if a <= 0:
+                n = max(0, ks.shape[1] + a)
+                self.held[s] = [ks[:, :n], vs[:, :n]]
+                continue
+            self.held[s] = ks, vs = [np.concatenate([x, y[:, at:at + a]], 1) for x, y in zip((ks, vs), (kq, vq))]
+            n = ks.shape[1]
+            assert int(new.lens[s]) == n
+            sees = np.arange(n)[None] < np.minimum((np.arange(n - a, n) // granule + 1) * granule, n)[:, None]
+            for h in range(self.Hq):
+                kk, vv = ks[h // (self.Hq // self.Hk)], vs[h // (self.Hq // self.Hk)]
+                ref, spread, reach = ora.attend(f64(q[h, at:at + a]), kk, vv, sees)
+                for r in range(a):
+                    tol = tolerance(self.dtype, f64(q[h, at + r]), kk, ref[r], spread[r], reach[r])
+                    assert (np.abs(f64(out[h, at + r]) - ref[r]) <= tol).all(), (s, h, r)
+            at += a
+
+
+STEPS = [[70, 3, 0, 130], [1, 1, 1, 1], [1, -1, 5, -130], [40, 1, 1, 64], [-1000, 2, 1, 1], [65, 1, -2, 1]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,Hq,Hk,interleaved", [(128, 4, 2, False), (64, 3, 1, True)])
+def test_serving_steps(dev, dtype, d, Hq, Hk, interleaved):
+    server = Server(dev, dtype, d, Hq, Hk, 4, 6, 12, d, interleaved)
+    for add in STEPS:
+        qkv = server.qkv(max(1, sum(max(a, 0) for a in add)))
+        got = server.step(qkv, i32(add, dev))
+        server.check(qkv, add, *got)
+        server.lens, server.state = got[0].lens, got[0].state
+
+
+def test_frames_match_the_dense_forward(dev):
+    """Frame by frame through the cache against the framework's own frame-causal forward on the values that the cache holds."""
+    d, H, frame, frames = 128, 3, 90, 4
+    N = frame * frames
+    server = Server(dev, "bf16", d, H, H, 1, 8, 8, 4, True)
+    outs, qs, ks, vs = [], [], [], []
+    for f in range(frames):
+        qkv = server.qkv(frame)
+        new, q, k, out = server.step(qkv, i32([frame], dev), granule=frame)
+        server.lens, server.state = new.lens, new.state
+        hk, hv = sc.read(server.store, new.slots)
+        outs.append(out), qs.append(q), ks.append(hk), vs.append(hv)
+    q, k, v = (torch.cat(x, 1)[None].contiguous() for x in (qs, ks, vs))
+    dense = sb.forward(q, k, v, 128, 64, 0.0, "dense", causal_granule=frame)
+    a, b = f64(torch.cat(outs, 1)), f64(dense[0])
+    # two bf16 results of the same products: each is within 2^-8 of its value and 2^-9 of the values' reach
+    assert np.abs(a - b).max() <= 2 * (2.0 ** -8 * np.abs(b).max() + 2.0 ** -9 * np.abs(f64(v)).max())
+    assert np.linalg.norm(a - b) <= 2 * 2.0 ** -8 * np.linalg.norm(b)
+
+
+def test_captured_steps(dev):
+    """Two steps captured into two graphs that share a store: each replay against an eager step on the same inputs."""
+    S, Hq, Hk, d = 3, 4, 2, 128
+
+    def server():
+        s = Server(dev, "bf16", d, Hq, Hk, S, 6, 20, 3, False)
+        first = torch.randn(150, Hq + 2 * Hk, d, generator=torch.Generator().manual_seed(1)).bfloat16().to(dev)
+        new, *_ = s.step(first, i32([100, 30, 20], dev))
+        s.lens, s.state = new.lens.clone(), new.state.clone()
+        return s
+    a, b = server(), server()
+    stream = torch.cuda.Stream()
+    graphs = []
+    for rows, add in ((3, [1, 1, 1]), (12, [4, 0, 7])):
+        qkv, adds = torch.zeros(rows, Hq + 2 * Hk, d, dtype=torch.bfloat16, device=dev), i32(add, dev)
+        with torch.cuda.stream(stream):
+            a.step(qkv, adds * 0)                                # a step that adds nothing, before the capture
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            new, q, k, out = a.step(qkv, adds)
+            a.lens.copy_(new.lens)
+            a.state.copy_(new.state)
+        graphs.append((graph, qkv, adds, out, new))
+    for turn in range(6):
+        graph, qkv, adds, out, new = graphs[turn % 2]
+        rows = qkv.shape[0]
+        x = torch.randn(qkv.shape, generator=torch.Generator().manual_seed(10 + turn)).bfloat16().to(dev)
+        if turn == 4:
+            adds.copy_(i32([1, -60, 1], dev))                    # a step of fewer rows than were captured
+        live = int(adds.clamp(min=0).sum())
+        qkv.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, _, _, eager = b.step(x, adds.clone())
+        b.lens, b.state = want.lens.clone(), want.state.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:, :live], eager[:, :live]), turn
+        assert torch.equal(new.slots, want.slots) and torch.equal(a.lens, b.lens) and torch.equal(a.state, b.state)
+        assert live <= rows
+
+
+def test_streams_of_their_own(dev):
+    """Calls on two other streams at once, each with its own workspace."""
+    rng = np.random.default_rng(2)
+    store, _, _ = make_store(rng, 40, 2, 128, dev)
+    torch.cuda.synchronize()
+    table, lens, row_start, positions = i32([list(range(40))], dev), i32([2500], dev), i32([0, 2], dev), i32([2498, 2499], dev)
+    qs = [torch.randn(4, 2, 128, generator=torch.Generator().manual_seed(i)).to(dev) for i in range(2)]
+    want = [sc.forward(q, store, table, lens, row_start, positions) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(sc.forward(qs[i], store, table, lens, row_start, positions))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i])
