@@ -1,20 +1,23 @@
 // Attention over the 4-bit cache.
 //
-// S^T = K Q^T and O^T = V^T P^T on 32 x 32 tiles, keys respectively channels on the rows and query rows on the lanes
-// (lane l: column l & 31, half h = l >> 5).  A query row is a (token, query head of the group) pair of one key/value head.
+// S^T = K Q^T and O^T = V^T P^T, keys respectively channels on the rows of the matrix tiles and query rows on the lanes.  A query
+// row is a (token, query head of the group) pair of one key/value head.
 //
-//   q . k   v_mfma_scale_f32_32x32x64_f8f6f4 takes the codes of the cache as they lie in memory, with their scales.  Its
-//           other operand holds q as a sum of 6-bit floats (e2m3, four significant bits each, every term at a sixteenth of the
-//           scale of the one before): three terms for bf16, which has eight significant bits, six for f32.  6-bit operands run at
-//           twice the rate of 8-bit ones (32 against 64 cycles), and the products of two terms with narrow exponents are summed
-//           without loss, which those of 8-bit floats are not.
-//   p . v   values are converted to f16 (exact), probabilities to f16 too: v_mfma_f32_32x32x16_f16.
+//   q . k   v_mfma_scale_f32_*_f8f6f4 takes the codes of the cache as they lie in memory, with their scales.  Its other operand
+//           holds q as a sum of 6-bit floats (e2m3, four significant bits each, every term at a sixteenth of the scale of the one
+//           before): three terms for bf16, which has eight significant bits, six for f32.  6-bit operands run at twice the
+//           rate of 8-bit ones (32 against 64 cycles for 32 x 32 x 64), and sums of their products lose nothing, where those
+//           of 8-bit floats, whose exponents reach further, were off by 2^-15 of the largest product.
+//   p . v   values are converted to f16 (exact), probabilities to f16 too: v_mfma_f32_*_f16.
 //
-// Row i of a key tile is key i with bits 2 and 3 exchanged: the accumulator registers of a lane then are the eight consecutive
-// keys that its half of the second product's operand wants, and P never leaves its lane.
+// Two kernels.  Requests of few rows: a wave takes 16 rows and a share of the keys, bytes of the cache go from memory to
+// registers (cache_few_kernel).  Others: four waves of 32 rows share tiles in LDS, whose values are converted
+// once for the 128 rows (cache_many_kernel).  Both cut the work of all requests into pieces of about the same number of pages,
+// whose partial results cache_join_kernel joins in the order of the keys.
 #include "sol_cache_internal.h"
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 namespace sol {
@@ -30,115 +33,137 @@ typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kTile = 32;             // query rows of a wave
-constexpr int kUnits = 2048;          // pieces of work that a launch aims at: 8 waves a compute unit
-constexpr int kLeastPages = 2;        // least pages of a piece
-constexpr float kShift = 7.0f;        // probabilities are held as 2^7 p: f16 keeps all bits down to 2^-21 of the maximum's
-constexpr float kSlack = 8.0f;        // log2 by which a logit may pass the running maximum before it is raised (2^15 < 65504)
+constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
+constexpr int kFewRows = 48;                    // a request of more goes to cache_many_kernel
+constexpr int kFewUnits = 3072;                 // pieces that a launch aims at: 12 waves a compute unit
+constexpr int kManyUnits = 1024;                // two workgroups a compute unit, twice
+constexpr int kLeastPages = 2;                  // least pages of a piece
+constexpr int kSlackPieces = 64;                // the mean number of pages is formed in f32
+constexpr float kShift = 7.0f;   // probabilities are held as 2^7 p: f16 keeps all bits down to 2^-21 of the maximum's
+constexpr float kSlack = 8.0f;   // log2 by which a logit may pass the running maximum before it is raised (2^15 < 65504)
 constexpr float kLowest = -3.402823466e38f;
 
 // The piece of work of one workgroup.
 struct Piece {
     int s, hk, tile, chunk, chunks;   // request, key/value head, tile of query rows, share of the keys
     int p0, p1;                       // pages
-    int row0, rows, len;              // rows of the request: the first one, and how many (token, head) pairs
-    long long slot0;                  // piece number of share 0 of this tile
+    int row0, rows, len;              // the request's first row, its (token, head) pairs of a key/value head, its length
+    int tiles;
+    unsigned slot0;                   // piece number of share 0 of this tile; shares lie `tiles` apart
 };
 
 struct Request {
-    int row0, rows, len, pages, tiles;   // rows: (token, head) pairs of a key/value head
+    int row0, rows, len, pages, tiles;
 };
 
-__device__ __forceinline__ Request request(const CacheAttnArgs& a, int s, int G) {
+// Requests with rows in (LO, HI] take part.
+struct Part {
+    int tile, units, lo, hi;
+};
+
+__device__ __forceinline__ Request request(const CacheAttnArgs& a, const Part& part, int s, int G) {
     Request r;
     const int first = min(max(a.row_start[s], 0), a.T), last = min(max(a.row_start[s + 1], first), a.T);
     r.row0 = first;
     r.rows = min(last - first, a.max_rows) * G;
+    if (r.rows <= part.lo || r.rows > part.hi) r.rows = 0;
     r.len = min(max(a.lens[s], 0), a.max_pages * kPage);
     r.pages = max((r.len + kPage - 1) / kPage, 1);
-    r.tiles = (r.rows + kTile - 1) / kTile;
+    r.tiles = (r.rows + part.tile - 1) / part.tile;
     return r;
 }
 
-// Pages of a piece: every tile of every request is cut into pieces of about the same number of pages, kUnits pieces in all
-// (and one more a tile at most).  By the lanes of one wave.
-__device__ __forceinline__ int pages_of_piece(const CacheAttnArgs& a, int G) {
-    const int lane = threadIdx.x & 63;
-    long long sum = 0;
-    for (int s = lane; s < a.S; s += 64) {
-        const Request r = request(a, s, G);
-        sum += (long long)r.tiles * r.pages;
-    }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
-    return (int)max((sum * a.Hk + kUnits - 1) / kUnits, (long long)kLeastPages);
+// Inclusive sum over the lanes of a wave.
+template <class T>
+__device__ __forceinline__ T scan_add(T x) {
+    static_assert(sizeof(T) == 4, "");
+#define SOL_STEP(ctrl, rows)                                                                                           \
+    x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, rows, 0xf, false))
+    SOL_STEP(0x111, 0xf);   // one to eight lanes to the right inside rows of 16
+    SOL_STEP(0x112, 0xf);
+    SOL_STEP(0x114, 0xf);
+    SOL_STEP(0x118, 0xf);
+    SOL_STEP(0x142, 0xa);   // the last lane of rows 0 and 2 to rows 1 and 3
+    SOL_STEP(0x143, 0xc);   // lane 31 to rows 2 and 3
+#undef SOL_STEP
+    return x;
 }
 
-// Piece `id` (BY_TILE: tile `id`, its share 0) of the launch; false past the last.  Pieces go by request, head, share, tile.
+template <class T>
+__device__ __forceinline__ T at_lane(T x, int lane) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
+// Every tile of every request is cut into pieces of about the same number of pages: `units` pieces in all, and one more a tile
+// at most.  Piece `id` (BY_TILE: share 0 of tile `id`); false past the last.  Pieces go by request, head, share, tile.  By the
+// lanes of one wave, on values that all waves of the launch and of the join see alike.
 template <bool BY_TILE>
-__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, int G, long long id, Piece& out) {
-    const int lane = threadIdx.x & 63;
-    const int per = pages_of_piece(a, G);
-    long long base = 0, slots = 0;   // pieces (tiles) and pieces before this round's requests
+__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& part, unsigned id, bool spread, Piece& out) {
+    const int lane = threadIdx.x & 63, G = a.Hq / a.Hk;
+    float sum = 0.f;
+    Request r = {};
+    for (int s = lane; s < a.S; s += 64) {
+        r = request(a, part, s, G);   // of up to 64 requests, each lane's own
+        sum += (float)r.tiles * (float)r.pages;
+    }
+    const float all = at_lane(scan_add(sum), 63);
+    const int per = (int)fmaxf(ceilf(all * (float)a.Hk / (float)part.units), (float)kLeastPages);
+    if (spread) {
+        // neighbouring workgroups run on different dies: give each die a run of neighbouring pieces, which share keys
+        unsigned total = 0;
+        for (int s = lane; s < a.S; s += 64) {
+            if (a.S > 64) r = request(a, part, s, G);
+            total += (unsigned)(r.tiles * ((r.pages + per - 1) / per)) * a.Hk;
+        }
+        total = at_lane(scan_add(total), 63);
+        const unsigned run = (total + 7) / 8;
+        if (id / 8 >= run) return false;
+        id = (id % 8) * run + id / 8;
+    }
+    unsigned base = 0, slots = 0;   // pieces (tiles) and pieces before this round's requests
     for (int s0 = 0; s0 < a.S; s0 += 64) {
         const int s = s0 + lane;
-        Request r = {};
-        int chunks = 0;
-        if (s < a.S) {
-            r = request(a, s, G);
-            chunks = (r.pages + per - 1) / per;
-        }
-        const long long pieces = (long long)r.tiles * chunks * a.Hk;
-        const long long mine = BY_TILE ? (long long)r.tiles * a.Hk : pieces;
-        long long upto = mine, slot_upto = pieces;
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            const long long x = __shfl_up(upto, m), y = __shfl_up(slot_upto, m);
-            if (lane >= m) upto += x, slot_upto += y;
-        }
+        if (a.S > 64) r = s < a.S ? request(a, part, s, G) : Request{};
+        const int chunks = (r.pages + per - 1) / per;
+        const unsigned pieces = (unsigned)(r.tiles * chunks) * a.Hk;
+        const unsigned mine = BY_TILE ? (unsigned)r.tiles * a.Hk : pieces;
+        const unsigned slot_upto = scan_add(pieces), upto = BY_TILE ? scan_add(mine) : slot_upto;
         const uint64_t hit = __ballot(base + upto > id);
         if (hit) {
             const int l = __builtin_ctzll(hit);
-            const long long within = id - (base + __shfl(upto - mine, l));
+            const unsigned within = id - (base + at_lane(upto - mine, l));
             out.s = s0 + l;
-            out.row0 = __shfl(r.row0, l);
-            out.rows = __shfl(r.rows, l);
-            out.len = __shfl(r.len, l);
-            const int tiles = __shfl(r.tiles, l), pages = __shfl(r.pages, l);
-            out.chunks = __shfl(chunks, l);
-            const long long first = slots + __shfl(slot_upto - pieces, l);
-            if (BY_TILE) {
-                out.hk = (int)(within / tiles);
-                out.tile = (int)(within % tiles);
-                out.chunk = 0;
-            } else {
-                out.hk = (int)(within / ((long long)tiles * out.chunks));
-                const int rest = (int)(within % ((long long)tiles * out.chunks));
-                out.chunk = rest / tiles;
-                out.tile = rest % tiles;
-            }
-            out.slot0 = first + (long long)out.hk * tiles * out.chunks + out.tile;
+            out.row0 = at_lane(r.row0, l);
+            out.rows = at_lane(r.rows, l);
+            out.len = at_lane(r.len, l);
+            out.tiles = at_lane(r.tiles, l);
+            const int pages = at_lane(r.pages, l);
+            out.chunks = at_lane(chunks, l);
+            const unsigned tiles = out.tiles, each = BY_TILE ? tiles : tiles * out.chunks;
+            if (each == 0) return false;
+            out.hk = (int)(within / each);
+            const unsigned rest = within % each;
+            out.chunk = (int)(rest / tiles);
+            out.tile = (int)(rest % tiles);
+            out.slot0 = slots + at_lane(slot_upto - pieces, l) + (unsigned)out.hk * tiles * out.chunks + out.tile;
             // equal shares of the pages
             out.p0 = (int)((long long)pages * out.chunk / out.chunks);
             out.p1 = (int)((long long)pages * (out.chunk + 1) / out.chunks);
-            return true;
+            return out.hk < a.Hk && out.chunk < out.chunks;   // rows that overlap may wrap the sums
         }
-        base += __shfl(upto, 63);
-        slots += __shfl(slot_upto, 63);
+        base += at_lane(upto, 63);
+        slots += at_lane(slot_upto, 63);
     }
     return false;
 }
 
-// Shares of one tile lie `tiles` pieces apart.
-__device__ __forceinline__ int tiles_of(const Piece& p) { return (p.rows + kTile - 1) / kTile; }
-
 // ---------------------------------------------------------------------------
-// Query rows: 32 channels of a lane's row, as terms of 6-bit floats.
+// Query rows: 32 channels of a lane's row, as terms of 6-bit floats.  Byte t of the scales is that of term t.
 // ---------------------------------------------------------------------------
 template <int NT>
 struct Split {
     u32x6 w[NT];
-    int scale[NT];
+    uint32_t scale[(NT + 3) / 4];
 };
 
 template <int NT>
@@ -155,14 +180,20 @@ __device__ __forceinline__ Split<NT> split_row(const float (&x)[32]) {
     for (int i = 0; i < 16; ++i) even[i] = x[2 * i], odd[i] = x[2 * i + 1];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const float scale = __uint_as_float((uint32_t)(e + 127 - 4 * t) << 23);
+        const uint32_t byte = e + 127 - 4 * t;
+        const float scale = __uint_as_float(byte << 23);
         r.w[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
-        r.scale[t] = top >= 0x7f800000u ? 255 : e + 127 - 4 * t;   // infinities and NaN make the row NaN
+        if (t % 4 == 0) r.scale[t / 4] = 0;
+        r.scale[t / 4] |= byte << (8 * (t % 4));
         if (t + 1 < NT) {
             const f32x32 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.w[t], scale);
 #pragma unroll
             for (int i = 0; i < 16; ++i) even[i] -= y[2 * i], odd[i] -= y[2 * i + 1];
         }
+    }
+    if (top >= 0x7f800000u) {   // infinities and NaN make the row NaN
+#pragma unroll
+        for (int i = 0; i < (NT + 3) / 4; ++i) r.scale[i] = ~0u;
     }
     return r;
 }
@@ -231,93 +262,457 @@ __device__ __forceinline__ void store_run(void* out, long long at, f32x4 v, int 
     }
 }
 
-__device__ __forceinline__ int swap23(int i) { return (i & 19) | ((i & 4) << 1) | ((i & 8) >> 1); }
-
-// One page's bytes, as a lane holds them.
-template <int D>
-struct PageRegs {
-    u32x4 k[2][D / 64];      // [32-key window][64-channel chunk]: 32 channels of one key
-    u32x4 v[4];              // [16-key step]: eight keys of D / 32 channels (d = 64: eight bytes)
-    u32x2 vs[4];             // their eight scales
-    uint32_t ks;             // scale bytes [chunk][window]
-};
-
-template <int D>
-__device__ __forceinline__ void load_page(const uint8_t* page, PageRegs<D>& r) {
-    using L = PageLayout<D>;
-    const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
-#pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c)
-            r.k[w][c] = *reinterpret_cast<const u32x4*>(page + L::k + (32 * w + swap23(i)) * (D / 2) + (2 * c + h) * 16);
-    if constexpr (D == 128) r.ks = *reinterpret_cast<const uint32_t*>(page + L::ks + lane * 4);
-    else r.ks = *reinterpret_cast<const uint16_t*>(page + L::ks + lane * 2);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int oct = 2 * u + h;
-        if constexpr (D == 128) {
-            r.v[u] = *reinterpret_cast<const u32x4*>(page + L::v + (oct * 32 + i) * 16);
-        } else {
-            const u32x2 x = *reinterpret_cast<const u32x2*>(page + L::v + (oct * 32 + i) * 8);
-            r.v[u] = u32x4{x[0], x[1], 0, 0};
-        }
-        r.vs[u] = *reinterpret_cast<const u32x2*>(page + L::vs + (oct * (D / 32) + i / (1024 / D)) * 8);
-    }
-}
-
-// The eight keys' f16 values of channel tile t (channels D/32 i + t), from a lane's bytes of a 16-key step.
-template <int D>
-__device__ __forceinline__ void values_f16(const u32x4 v, const float (&scale)[8], f16x8 (&out)[D / 32]) {
+// Eight f16 values (keys) of each channel of a lane's bytes: `n` dwords of a key's codes interleaved as in the cache.  BYTES: bytes
+// of a key (two channels each).  scale[k]: exponent of key k, as a float of which the conversion reads the exponent only.
+template <int BYTES>
+__device__ __forceinline__ void values_f16(const u32x4 v, const float (&scale)[8], f16x8 (&out)[2 * BYTES]) {
+#define SOL_CVT(w, s, sel) __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, sel)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {   // keys 2j, 2j + 1
 #pragma unroll
-        for (int b = 0; b < D / 64; ++b) {
+        for (int b = 0; b < BYTES; ++b) {
             f16x2 x, y;
-            if constexpr (D == 128) {
-                x = b ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j], scale[2 * j], 1) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j], scale[2 * j], 0);
-                y = b ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j], scale[2 * j + 1], 3) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j], scale[2 * j + 1], 2);
+            if constexpr (BYTES == 2) {
+                x = b ? SOL_CVT(v[j], scale[2 * j], 1) : SOL_CVT(v[j], scale[2 * j], 0);
+                y = b ? SOL_CVT(v[j], scale[2 * j + 1], 3) : SOL_CVT(v[j], scale[2 * j + 1], 2);
             } else {
-                x = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j >> 1], scale[2 * j], 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j >> 1], scale[2 * j], 0);
-                y = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j >> 1], scale[2 * j + 1], 3) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[j >> 1], scale[2 * j + 1], 1);
+                x = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j], 2) : SOL_CVT(v[j >> 1], scale[2 * j], 0);
+                y = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j + 1], 3) : SOL_CVT(v[j >> 1], scale[2 * j + 1], 1);
             }
             out[2 * b][2 * j] = x[0], out[2 * b][2 * j + 1] = y[0];
             out[2 * b + 1][2 * j] = x[1], out[2 * b + 1][2 * j + 1] = y[1];
         }
     }
+#undef SOL_CVT
 }
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ __forceinline__ void scales_of(u32x2 b, float (&scale)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        scale[4 * i + 0] = __uint_as_float(b[i] << 23);
+        scale[4 * i + 1] = __uint_as_float(b[i] << 15);
+        scale[4 * i + 2] = __uint_as_float(b[i] << 7);
+        scale[4 * i + 3] = __uint_as_float(b[i] >> 1);
+    }
+}
+
+// Probabilities as f16 operands: cut to f16 (F32T: two terms), and their sum as cut added to l.
+template <bool F32T>
+__device__ __forceinline__ void cut_pair(float e0, float e1, f16x8& hi, f16x8& lo, int i, float& l) {
+    const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e0, e1));
+    hi[2 * i] = h[0], hi[2 * i + 1] = h[1];
+    l = __builtin_amdgcn_fdot2(h, f16x2{1, 1}, l, false);
+    if constexpr (F32T) {
+        const f16x2 r = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e0 - (float)h[0], e1 - (float)h[1]));
+        lo[2 * i] = r[0], lo[2 * i + 1] = r[1];
+        l = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l, false);
+    }
+}
+
+__device__ __forceinline__ int row_limit(const CacheAttnArgs& a, int token, int len) {
+    const int pos = a.positions[token];
+    return pos < 0 ? 0 : (int)min(((long long)pos / a.granule + 1) * a.granule, (long long)len);
+}
+
+// The next page that is there, from p on.
+__device__ __forceinline__ bool next_page(const int* table, int P, int p1, int& p, int& id) {
+    while (p < p1) {
+        id = table[p];
+        if (id >= 0 && id < P) return true;
+        ++p;
+    }
+    return false;
+}
 
 // ---------------------------------------------------------------------------
-// A wave a piece: 32 query rows against pages [p0, p1).  Both sums of a row run over the page's keys in registers; the next page's
-// bytes are loaded while this one's are used.
+// Few rows: a wave a piece, 16 query rows (lane l: row l & 15) against pages [p0, p1).  Bound by the bytes of the cache.  Lane
+// group g = l >> 4 holds channels 32g ... of the keys (16 x 16 x 128: one scale a lane; at d = 64 the upper groups hold
+// zeros).  Row 4g + e of key tile b of a 32-key window is key 8g + 4b + e: registers e of the tiles 0 and 1 are then the
+// eight consecutive keys that group g holds of the second product's operand.  Registers are filled again as soon as they
+// are used: the keys of the next page are on their way during the second product, its values during the next first one.
 // ---------------------------------------------------------------------------
-template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64) void cache_attn_kernel(const CacheAttnArgs a, const float scale_log2) {
+template <int D>
+struct FewPage {
+    u32x4 k[4];            // [2 w + b]
+    u32x4 v[2][D / 64];    // [w]: eight keys of D / 16 channels
+    u32x2 vs[2];
+    uint32_t ks;           // byte 2 b + w
+};
+
+template <int D>
+__device__ __forceinline__ void few_load_k(const uint8_t* page, FewPage<D>& r) {
     using L = PageLayout<D>;
-    constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
-    const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int key = 8 * (i >> 2) + (i & 3);
+    if (D == 64 && g >= 2) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) r.k[t] = u32x4{0, 0, 0, 0};
+        r.ks = 0x7f7f7f7fu;
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+        r.k[t] = *reinterpret_cast<const u32x4*>(page + L::k + (32 * (t >> 1) + key + 4 * (t & 1)) * (D / 2) + 16 * g);
+    // scale of (key, group g) at [g & 1][key with bits 2 and 3 exchanged][g >> 1][w]
+    const int at = ((g & 1) * 32 + 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3)) * (D / 32) + (g >> 1) * 2;
+    r.ks = *reinterpret_cast<const uint16_t*>(page + L::ks + at) |
+           ((uint32_t)*reinterpret_cast<const uint16_t*>(page + L::ks + at + 8 * (D / 32)) << 16);
+}
+
+template <int D>
+__device__ __forceinline__ void few_load_v(const uint8_t* page, FewPage<D>& r) {
+    using L = PageLayout<D>;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)   // 32 bytes (d = 64: 16) of two channel runs
+            r.v[w][c] = *reinterpret_cast<const u32x4*>(page + L::v + ((4 * w + g) * 32 + 2 * i) * (D / 8) + 16 * c);
+        r.vs[w] = *reinterpret_cast<const u32x2*>(page + L::vs + ((4 * w + g) * (D / 32) + i / (512 / D)) * 8);
+    }
+}
+
+template <int D, bool F32T, bool EDGE>
+__device__ __forceinline__ void few_first(const FewPage<D>& pg, const Split<F32T ? 6 : 3>& q, int key0, int sees, f32x4 (&s)[4]) {
+    constexpr int NT = F32T ? 6 : 3;
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#define SOL_MFMA(t, ks_byte, n, q_byte)                                                                                   \
+    s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i32x8{(int)pg.k[t][0], (int)pg.k[t][1], (int)pg.k[t][2], (int)pg.k[t][3], 0, 0, 0, 0},   \
+                                                            i32x8{(int)q.w[n][0], (int)q.w[n][1], (int)q.w[n][2], (int)q.w[n][3], (int)q.w[n][4], (int)q.w[n][5], 0, 0}, \
+                                                            s[t], 4, 2, ks_byte, (int)pg.ks, q_byte, (int)q.scale[(n) / 4])
+#define SOL_TERM(n, q_byte) SOL_MFMA(0, 0, n, q_byte), SOL_MFMA(1, 2, n, q_byte), SOL_MFMA(2, 1, n, q_byte), SOL_MFMA(3, 3, n, q_byte)
+    SOL_TERM(0, 0);
+    SOL_TERM(1, 1);
+    SOL_TERM(2, 2);
+    if constexpr (NT == 6) {
+        SOL_TERM(3, 3);
+        SOL_TERM(4, 0);
+        SOL_TERM(5, 1);
+    }
+#undef SOL_TERM
+#undef SOL_MFMA
+    if constexpr (EDGE) {
+        const int left = sees - key0 - 8 * g;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (32 * (t >> 1) + 4 * (t & 1) + e >= left) s[t][e] = -INFINITY;
+    }
+}
+
+template <int D, bool F32T, bool EDGE>
+__device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], int key0, int most, float scale_log2, float& m, float& l,
+                                           f32x4 (&o)[D / 16]) {
+    const int g = (threadIdx.x & 63) >> 4;
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
+    top *= scale_log2;
+    // lanes of a row that lags behind see it in their own part first: the vote is over all of them
+    if (__any(top > m + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float up = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - up);
+        m = up;
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
+    }
+    const float off = kShift - m;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        f16x8 ph = {}, pl = {};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                cut_pair<F32T>(__builtin_amdgcn_exp2f(fmaf(s[2 * w + b][2 * e], scale_log2, off)),
+                               __builtin_amdgcn_exp2f(fmaf(s[2 * w + b][2 * e + 1], scale_log2, off)), ph, pl, 2 * b + e, l);
+        float vs[8];
+        scales_of(pg.vs[w], vs);
+        if constexpr (EDGE) {   // what lies behind the last token may be anything: a finite scale keeps 0 v = 0
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (key0 + 32 * w + 8 * g + i >= most) vs[i] = 1.0f;
+        }
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+            // 16 bytes: eight keys of two bytes (d = 128), or two runs of eight bytes (d = 64)
+            f16x8 va[4];
+            if constexpr (D == 128) {
+                values_f16<2>(pg.v[w][c], vs, va);
+            } else {
+                f16x8 x[2], y[2];
+                values_f16<1>(u32x4{pg.v[w][c][0], pg.v[w][c][1], 0, 0}, vs, x);
+                values_f16<1>(u32x4{pg.v[w][c][2], pg.v[w][c][3], 0, 0}, vs, y);
+                va[0] = x[0], va[1] = x[1], va[2] = y[0], va[3] = y[1];
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                o[4 * c + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[t], ph, o[4 * c + t], 0, 0, 0);
+                if constexpr (F32T) o[4 * c + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[t], pl, o[4 * c + t], 0, 0, 0);
+            }
+        }
+    }
+}
+
+template <int D, bool F32T, bool VEC>
+__global__ __launch_bounds__(64, F32T ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2) {
+    using L = PageLayout<D>;
+    constexpr int NT = F32T ? 6 : 3, CT = D / 16;
+    const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece<false>(a, G, blockIdx.x, pc)) return;
+    if (!find_piece<false>(a, part, blockIdx.x, false, pc)) return;
 
-    // this lane's query row
-    const int r = pc.tile * kTile + j;
+    const int r = pc.tile * kFewTile + j;
     const bool valid = r < pc.rows;
     const int token = pc.row0 + (valid ? r / G : 0), head = pc.hk * G + (valid ? r % G : 0);
-    const int pos = a.positions[token];
-    int sees = 0;
-    if (pos >= 0) sees = (int)min(((long long)pos / a.granule + 1) * a.granule, (long long)pc.len);
+    const int sees = row_limit(a, token, pc.len);
+    float x[32];
+    if (D == 128 || g < 2) {
+        load_row<F32T, VEC>(a.q, head * a.sq.h + token * a.sq.n + 32 * g, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = 0.f;
+    }
+    int most = sees, least = sees;
+#pragma unroll
+    for (int m = 1; m < 16; m *= 2) {
+        most = max(most, __shfl_xor(most, m));
+        least = min(least, __shfl_xor(least, m));
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(least);
+    const int p1 = min(pc.p1, (most + kPage - 1) / kPage);
+    const int* table = a.table + (long long)pc.s * a.max_pages;
+    const long long page_stride = (long long)a.Hk * L::bytes;
+    const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
+
+    f32x4 o[CT], s[4];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = kLowest, l = 0.f;
+    FewPage<D> pg;
+    int p = pc.p0, id = 0;
+    bool more = next_page(table, a.P, p1, p, id);
+    const uint8_t* page = store + id * page_stride;
+    if (more) {
+        few_load_k<D>(page, pg);
+        few_load_v<D>(page, pg);
+    }
+    const Split<NT> q = split_row<NT>(x);
+    while (more) {
+        const int key0 = p * kPage;
+        ++p;
+        more = next_page(table, a.P, p1, p, id);
+        const bool edge = key0 + kPage > least;
+        if (edge) few_first<D, F32T, true>(pg, q, key0, sees, s);
+        else few_first<D, F32T, false>(pg, q, key0, sees, s);
+        if (more) {
+            page = store + id * page_stride;
+            few_load_k<D>(page, pg);
+        }
+        if (edge) few_second<D, F32T, true>(pg, s, key0, most, scale_log2, m, l, o);
+        else few_second<D, F32T, false>(pg, s, key0, most, scale_log2, m, l, o);
+        if (more) few_load_v<D>(page, pg);
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (!valid) return;
+    // register e of channel tile t is channel CT (4g + e) + t
+    if (pc.chunks == 1) {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        const long long oi = head * a.so.h + token * a.so.n;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t = 0; t < CT; t += 4)
+                store_run<F32T, VEC>(a.out, oi + CT * (4 * g + e) + t, f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]} * inv, 4);
+        return;
+    }
+    float* to = static_cast<float*>(a.ws) + (long long)blockIdx.x * (kFewTile * (D + 2));
+    if (g == 0) to[2 * j] = m, to[2 * j + 1] = l;
+    float* po = to + 2 * kFewTile + j * D;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < CT; t += 4)
+            *reinterpret_cast<f32x4*>(po + CT * (4 * g + e) + t) = f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]};
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: four waves of 32 query rows (lane l: row l & 31, half h = l >> 5) on one piece.  A page lies in LDS as operands: the
+// codes of the keys as they are (32 x 32 x 64: a lane's 32 channels of a key), the values as f16, converted by thread t for eight
+// keys of D / 32 channels.  Two stages: while a page is used, the next one is converted from registers, and the one after is on its
+// way.  Row i of a 32-key window is key i with bits 2 and 3 exchanged, so that the registers 8u ... 8u + 7 of the first
+// product are the eight consecutive keys that a lane holds of the second one's operand.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ int swap23(int i) { return (i & 19) | ((i & 4) << 1) | ((i & 8) >> 1); }
+
+template <int D>
+struct Stage {
+    u32x4 k[2 * (D / 64) * 64];     // [window][64-channel chunk][lane]
+    f16x8 v[4 * (D / 32) * 64];     // [16-key step][channel tile][lane]
+    uint32_t ks[64];                // scale bytes [chunk][window] of a lane
+};
+
+template <int D>
+struct ManyPage {                   // a thread's part of a page
+    u32x4 k, v;
+    u32x2 vs;
+    uint32_t ks;
+};
+
+template <int D>
+__device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D>& r) {
+    using L = PageLayout<D>;
+    const int t = threadIdx.x, lane = t & 63, i = lane & 31, h = lane >> 5;
+    if (D == 128 || t < 128) {
+        const int w = D == 128 ? t >> 7 : t >> 6, c = D == 128 ? (t >> 6) & 1 : 0;
+        r.k = *reinterpret_cast<const u32x4*>(page + L::k + (32 * w + swap23(i)) * (D / 2) + (2 * c + h) * 16);
+    }
+    // thread t: keys 8 (t >> 5) ..., channel run t & 31
+    if constexpr (D == 128) {
+        r.v = *reinterpret_cast<const u32x4*>(page + L::v + t * 16);
+    } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(page + L::v + t * 8);
+        r.v = u32x4{x[0], x[1], 0, 0};
+    }
+    r.vs = *reinterpret_cast<const u32x2*>(page + L::vs + ((t >> 5) * (D / 32) + (t & 31) / (1024 / D)) * 8);
+    if (t < 64) {
+        if constexpr (D == 128) r.ks = *reinterpret_cast<const uint32_t*>(page + L::ks + t * 4);
+        else r.ks = *reinterpret_cast<const uint16_t*>(page + L::ks + t * 2);
+    }
+}
+
+// most: tokens from here on of the page may be anything.
+template <int D>
+__device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, int most) {
+    constexpr int CT = D / 32;
+    const int t = threadIdx.x;
+    if (D == 128 || t < 128) st.k[t] = r.k;
+    if (t < 64) st.ks[t] = r.ks;
+    float vs[8];
+    scales_of(r.vs, vs);
+    if (most < kPage) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (8 * (t >> 5) + i >= most) vs[i] = 1.0f;
+    }
+    f16x8 va[CT];
+    values_f16<D / 64>(r.v, vs, va);
+    const int u = t >> 6, lane = t & 63;   // keys 16u + 8h ...
+#pragma unroll
+    for (int c = 0; c < CT; ++c) st.v[(u * CT + c) * 64 + lane] = va[c];
+}
+
+template <int D, bool F32T>
+__device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ? 6 : 3> (&q)[D / 64], int key0, bool edge, int sees,
+                                          float scale_log2, float& m, float& l, f32x16 (&o)[D / 32]) {
+    constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    f32x16 s[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[w][i] = 0.f;
+    const int ks = (int)st.ks[lane];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const u32x4 k0 = st.k[c * 64 + lane], k1 = st.k[(NC + c) * 64 + lane];
+#define SOL_MFMA(win, kk, ks_byte, n, q_byte)                                                                               \
+    s[win] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(i32x8{(int)kk[0], (int)kk[1], (int)kk[2], (int)kk[3], 0, 0, 0, 0}, \
+                                                           i32x8{(int)q[c].w[n][0], (int)q[c].w[n][1], (int)q[c].w[n][2], (int)q[c].w[n][3], (int)q[c].w[n][4], (int)q[c].w[n][5], 0, 0}, \
+                                                           s[win], 4, 2, ks_byte, ks, q_byte, (int)q[c].scale[(n) / 4])
+#define SOL_TERM(n, q_byte)                                                            \
+    do {                                                                               \
+        if (c == 0) SOL_MFMA(0, k0, 0, n, q_byte), SOL_MFMA(1, k1, 1, n, q_byte);      \
+        else SOL_MFMA(0, k0, 2, n, q_byte), SOL_MFMA(1, k1, 3, n, q_byte);             \
+    } while (0)
+        SOL_TERM(0, 0);
+        SOL_TERM(1, 1);
+        SOL_TERM(2, 2);
+        if constexpr (NT == 6) {
+            SOL_TERM(3, 3);
+            SOL_TERM(4, 0);
+            SOL_TERM(5, 1);
+        }
+#undef SOL_TERM
+#undef SOL_MFMA
+    }
+    // register 8u + 4b + e of window w is key 32w + 16u + 8h + 4b + e
+    if (edge) {
+        const int left = sees - key0 - 8 * h;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (32 * w + 16 * (i >> 3) + (i & 7) >= left) s[w][i] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[w][i]);
+    top *= scale_log2;
+    if (__any(top > m + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float up = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - up);
+        m = up;
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
+    }
+    const float off = kShift - m;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        f16x8 ph = {}, pl = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            cut_pair<F32T>(__builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + 2 * i], scale_log2, off)),
+                           __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + 2 * i + 1], scale_log2, off)), ph, pl, i, l);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const f16x8 va = st.v[(u * CT + t) * 64 + lane];
+            o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, ph, o[t], 0, 0, 0);
+            if constexpr (F32T) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pl, o[t], 0, 0, 0);
+        }
+    }
+}
+
+template <int D, bool F32T, bool VEC>
+__global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2, float* ws) {
+    using L = PageLayout<D>;
+    constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
+    __shared__ Stage<D> stage[2];
+    __shared__ int s_most[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, h = lane >> 5;
+    const int G = a.Hq / a.Hk;
+    Piece pc;
+    if (!find_piece<false>(a, part, blockIdx.x, true, pc)) return;   // alike in the four waves
+    const unsigned slot = pc.slot0 + (unsigned)pc.chunk * pc.tiles;
+
+    const int r = pc.tile * kManyTile + 32 * wave + j;
+    const bool valid = r < pc.rows, busy = pc.tile * kManyTile + 32 * wave < pc.rows;
+    const int token = pc.row0 + (valid ? r / G : 0), head = pc.hk * G + (valid ? r % G : 0);
+    int sees = row_limit(a, token, pc.len);
+    if (!valid) sees = 0;
     Split<NT> q[NC];
-    const long long qi = head * a.sq.h + token * a.sq.n;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         float x[32];
-        load_row<F32T, VEC>(a.q, qi + 64 * c + 32 * h, x);
+        load_row<F32T, VEC>(a.q, head * a.sq.h + token * a.sq.n + 64 * c + 32 * h, x);
         q[c] = split_row<NT>(x);
     }
-    int most = sees, least = sees;
+    int most = sees, least = valid ? sees : INT_MAX;
 #pragma unroll
     for (int m = 1; m < 32; m *= 2) {
         most = max(most, __shfl_xor(most, m));
@@ -325,11 +720,13 @@ __global__ __launch_bounds__(64) void cache_attn_kernel(const CacheAttnArgs a, c
     }
     most = __builtin_amdgcn_readfirstlane(most);
     least = __builtin_amdgcn_readfirstlane(least);
-    const int p0 = __builtin_amdgcn_readfirstlane(pc.p0);
-    const int p1 = min(__builtin_amdgcn_readfirstlane(pc.p1), (most + kPage - 1) / kPage);
-    const int* table = a.table + (long long)__builtin_amdgcn_readfirstlane(pc.s) * a.max_pages;
+    if (lane == 0) s_most[wave] = most;
+    __syncthreads();
+    const int all = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+    const int p1 = __builtin_amdgcn_readfirstlane(min(pc.p1, (all + kPage - 1) / kPage));
+    const int* table = a.table + (long long)pc.s * a.max_pages;
     const long long page_stride = (long long)a.Hk * L::bytes;
-    const uint8_t* store = a.store + (long long)__builtin_amdgcn_readfirstlane(pc.hk) * L::bytes;
+    const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
 
     f32x16 o[CT];
 #pragma unroll
@@ -338,117 +735,34 @@ __global__ __launch_bounds__(64) void cache_attn_kernel(const CacheAttnArgs a, c
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = kLowest, l = 0.f;
 
-    // the next page that is there, from p on
-    auto next = [&](int& p, int& id) {
-        while (p < p1) {
-            id = table[p];
-            if (id >= 0 && id < a.P) return true;
-            ++p;
-        }
-        return false;
-    };
-    int p = p0, id = 0;
-    PageRegs<D> cur;
-    bool more = next(p, id);
-    if (more) load_page<D>(store + id * page_stride, cur);
+    // page p is in stage[turn], page pn in registers
+    ManyPage<D> pg;
+    int p = pc.p0, id = 0;
+    bool more = next_page(table, a.P, p1, p, id);
+    int pn = p, turn = 0;
+    if (more) {
+        many_load<D>(store + id * page_stride, pg);
+        many_store<D>(pg, stage[0], pc.len - p * kPage);
+        ++pn;
+    }
+    bool more_n = more && next_page(table, a.P, p1, pn, id);
+    if (more_n) many_load<D>(store + id * page_stride, pg);
+    __syncthreads();
     while (more) {
         const int key0 = p * kPage;
-        ++p;
-        more = next(p, id);
-        PageRegs<D> nxt = cur;
-        if (more) load_page<D>(store + id * page_stride, nxt);
-
-        f32x16 s[2];
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[w][i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                i32x8 ka = {};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ka[i] = (int)cur.k[w][c][i];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    i32x8 qb = {};
-#pragma unroll
-                    for (int i = 0; i < 6; ++i) qb[i] = (int)q[c].w[t][i];
-                    switch (2 * c + w) {   // the byte of the key scales is an immediate
-                    case 0: s[w] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s[w], 4, 2, 0, (int)cur.ks, 0, q[c].scale[t]); break;
-                    case 1: s[w] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s[w], 4, 2, 1, (int)cur.ks, 0, q[c].scale[t]); break;
-                    case 2: s[w] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s[w], 4, 2, 2, (int)cur.ks, 0, q[c].scale[t]); break;
-                    default: s[w] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s[w], 4, 2, 3, (int)cur.ks, 0, q[c].scale[t]); break;
-                    }
-                }
-            }
+        p = pn;
+        more = more_n;
+        if (more) {
+            many_store<D>(pg, stage[turn ^ 1], pc.len - p * kPage);
+            ++pn;
+            more_n = next_page(table, a.P, p1, pn, id);
+            if (more_n) many_load<D>(store + id * page_stride, pg);
         }
-        // register 8u + 4b + e of window w is key 32w + 16u + 8h + 4b + e
-        const bool edge = key0 + kPage > least;
-        if (edge) {
-            const int left = sees - key0 - 8 * h;
-#pragma unroll
-            for (int w = 0; w < 2; ++w)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (32 * w + 16 * (i >> 3) + (i & 7) >= left) s[w][i] = -INFINITY;
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[w][i]);
-        top = fmaxf(top, other_half(top)) * scale_log2;
-        if (__any(top > m + kSlack)) {
-            const float up = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - up);
-            m = up;
-            l *= alpha;
-#pragma unroll
-            for (int t = 0; t < CT; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
-        }
-        const float off = kShift - m;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            f16x8 ph, pl;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float e[2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) e[x] = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + 2 * i + x], scale_log2, off));
-                const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e[0], e[1]));
-                ph[2 * i] = hi[0], ph[2 * i + 1] = hi[1];
-                l = __builtin_amdgcn_fdot2(hi, f16x2{1, 1}, l, false);
-                if constexpr (F32T) {
-                    const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e[0] - (float)hi[0], e[1] - (float)hi[1]));
-                    pl[2 * i] = lo[0], pl[2 * i + 1] = lo[1];
-                    l = __builtin_amdgcn_fdot2(lo, f16x2{1, 1}, l, false);
-                }
-            }
-            float vs[8];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {   // the conversion reads the exponent only
-                vs[4 * i + 0] = __uint_as_float(cur.vs[u][i] << 23);
-                vs[4 * i + 1] = __uint_as_float(cur.vs[u][i] << 15);
-                vs[4 * i + 2] = __uint_as_float(cur.vs[u][i] << 7);
-                vs[4 * i + 3] = __uint_as_float(cur.vs[u][i] >> 1);
-            }
-            if (key0 + kPage > most) {   // what lies behind the last token may be anything: a finite scale keeps 0 v = 0
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (key0 + 16 * u + 8 * h + i >= most) vs[i] = 1.0f;
-            }
-            f16x8 va[CT];
-            values_f16<D>(cur.v[u], vs, va);
-#pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va[t], ph, o[t], 0, 0, 0);
-                if constexpr (F32T) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va[t], pl, o[t], 0, 0, 0);
-            }
-        }
-        cur = nxt;
+        if (busy && key0 < most) many_page<D, F32T>(stage[turn], q, key0, key0 + kPage > least, sees, scale_log2, m, l, o);
+        turn ^= 1;
+        __syncthreads();
     }
-    l += other_half(l);
+    l += __shfl_xor(l, 32);
     if (!valid) return;
     // register i of channel tile t is channel CT (8 (i >> 2) + 4h + (i & 3)) + t
     if (pc.chunks == 1) {
@@ -463,10 +777,11 @@ __global__ __launch_bounds__(64) void cache_attn_kernel(const CacheAttnArgs a, c
         }
         return;
     }
-    const long long slot = pc.slot0 + (long long)pc.chunk * tiles_of(pc);   // blockIdx.x
-    float* part = static_cast<float*>(a.ws) + slot * (kTile * (D + 2));
-    if (h == 0) part[2 * j] = m, part[2 * j + 1] = l;
-    float* po = part + 2 * kTile + j * D;
+    if (slot >= gridDim.x) return;   // rows that overlap: no room was asked for
+    float* to = ws + (long long)slot * (kManyTile * (D + 2));
+    const int row = 32 * wave + j;
+    if (h == 0) to[2 * row] = m, to[2 * row + 1] = l;
+    float* po = to + 2 * kManyTile + row * D;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
 #pragma unroll
@@ -474,84 +789,146 @@ __global__ __launch_bounds__(64) void cache_attn_kernel(const CacheAttnArgs a, c
 }
 
 // ---------------------------------------------------------------------------
-// Joins the shares of a tile, in their order: a workgroup a tile, a wave a row at a time, D / 64 channels a lane.
+// Joins the shares of 16 rows of a tile in their order.  D / 4 threads a row and group of shares, four channels each: with few
+// rows the shares are dealt to several groups, whose sums are added in LDS.
 // ---------------------------------------------------------------------------
-template <int D, bool F32T>
-__global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a, const long long pieces) {
-    constexpr int CL = D / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <int D, bool F32T, bool VEC>
+__global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a, const Part part, const unsigned pieces, const float* ws) {
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ f32x4 s_o[GROUPS][LANES];
+    __shared__ float s_l[GROUPS];
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece<true>(a, G, blockIdx.x, pc) || pc.chunks == 1) return;
-    const int tiles = tiles_of(pc);
-    if (pc.slot0 + (long long)(pc.chunks - 1) * tiles >= pieces) return;   // rows that overlap: no room was asked for
-    const float* part = static_cast<const float*>(a.ws) + pc.slot0 * (kTile * (D + 2));
-    const long long stride = (long long)tiles * (kTile * (D + 2));
-    for (int j = wave; j < kTile; j += 4) {
-        const int r = pc.tile * kTile + j;
-        if (r >= pc.rows) break;
-        float top = kLowest;
-        for (int c = lane; c < pc.chunks; c += 64) top = fmaxf(top, part[c * stride + 2 * j]);
+    if (!find_piece<true>(a, part, blockIdx.x, false, pc) || pc.chunks == 1) return;
+    if (pc.slot0 + (uint64_t)(pc.chunks - 1) * pc.tiles >= pieces) return;   // rows that overlap: no room was asked for
+    const int first = pc.tile * part.tile + 16 * blockIdx.y, rows = min(pc.rows - first, 16);
+    if (rows <= 0) return;
+    const long long stride = (long long)pc.tiles * (part.tile * (D + 2));
+    const float* at = ws + (long long)pc.slot0 * (part.tile * (D + 2)) + 2 * 16 * blockIdx.y;   // (max, sum) pairs of the rows
+    const float* ot = ws + (long long)pc.slot0 * (part.tile * (D + 2)) + 2 * part.tile + 16 * blockIdx.y * D;
+    const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    // rows at a time: a power of two, so that the groups of a row are equally many
+    const int width = rows == 1 ? 1 : rows == 2 ? 2 : rows <= 4 ? 4 : min(GROUPS, 8), shares = GROUPS / width;
+    for (int j0 = 0; j0 < rows; j0 += width) {
+        const int j = j0 + group % width, share = group / width;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+        if (j < rows) {
+            float top = kLowest;
+            for (int c = lane; c < pc.chunks; c += LANES) top = fmaxf(top, at[c * stride + 2 * j]);
 #pragma unroll
-        for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-        float l = 0.f, o[CL] = {};
-        for (int c = 0; c < pc.chunks; ++c) {
-            const float* at = part + c * stride;
-            const float w = __builtin_amdgcn_exp2f(at[2 * j] - top);
-            l += w * at[2 * j + 1];
-#pragma unroll
-            for (int i = 0; i < CL; ++i) o[i] += w * at[2 * kTile + j * D + CL * lane + i];
+            for (int x = 1; x < LANES; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+#pragma unroll 4
+            for (int c = share; c < pc.chunks; c += shares) {
+                const float w = __builtin_amdgcn_exp2f(at[c * stride + 2 * j] - top);
+                l += w * at[c * stride + 2 * j + 1];
+                o += w * *reinterpret_cast<const f32x4*>(ot + c * stride + j * D + 4 * lane);
+            }
         }
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const long long oi = (pc.hk * G + r % G) * a.so.h + (pc.row0 + r / G) * a.so.n + CL * lane;
-#pragma unroll
-        for (int i = 0; i < CL; ++i) store_run<F32T, false>(a.out, oi + i, f32x4{o[i] * inv, 0.f, 0.f, 0.f}, 1);
+        if (shares > 1) {
+            __syncthreads();
+            s_o[group][lane] = o;
+            if (lane == 0) s_l[group] = l;
+            __syncthreads();
+            if (share == 0)
+                for (int x = 1; x < shares; ++x) o += s_o[group + x * width][lane], l += s_l[group + x * width];
+        }
+        if (j < rows && share == 0) {
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            const int r = first + j;
+            store_run<F32T, VEC>(a.out, (pc.hk * G + r % G) * a.so.h + (pc.row0 + r / G) * a.so.n + 4 * lane, o * inv, 4);
+        }
     }
 }
 
 // Tiles of a launch at most, whatever the lengths: a request's last tile may be part full.
-long long most_tiles(int S, int T, int max_rows, int Hq, int Hk) {
-    const long long rows = std::min((long long)T, (long long)S * max_rows) * (Hq / Hk);
-    return (rows / kTile + std::min(S, T)) * Hk;
+long long most_tiles(const Part& part, int S, int T, int max_rows, int Hq, int Hk) {
+    const int G = Hq / Hk;
+    const long long rows = std::min((long long)T, (long long)S * max_rows) * G;
+    // a request of this part has more than lo rows
+    const long long requests = std::min<long long>(std::min(S, T), rows / (part.lo + 1));
+    return (rows / part.tile + requests) * Hk;
 }
 
-// Pieces at most: pages_of_piece() rounds a piece's pages up, so a tile adds one to kUnits; and no tile has more than its pages give.
-long long most_pieces(int S, int T, int max_rows, int Hq, int Hk, int max_pages) {
-    const long long tiles = most_tiles(S, T, max_rows, Hq, Hk);
-    return std::min(tiles + kUnits, tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
+// Pieces at most: a piece's pages are rounded up, so a tile adds one to `units`; and no tile has more than its pages give.
+long long most_pieces(const Part& part, int S, int T, int max_rows, int Hq, int Hk, int max_pages) {
+    const long long tiles = most_tiles(part, S, T, max_rows, Hq, Hk);
+    return std::min(tiles + part.units + kSlackPieces, tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
+}
+
+struct Plan {
+    Part few, many;
+    bool use_few, use_many;
+    long long few_pieces, many_pieces, few_tiles, many_tiles;
+    size_t few_bytes, many_bytes;
+};
+
+// Which kernels a call needs: requests of up to kFewRows rows go to the one for few rows, unless there is one request only, whose
+// rows the caller bounds; where no request can have more, nothing goes to the other.
+Plan make_plan(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages) {
+    Plan p{};
+    const long long most = (long long)std::min(max_rows, T) * (Hq / Hk);
+    p.use_many = most > kFewRows;
+    p.use_few = !p.use_many || S > 1;
+    p.few = {kFewTile, kFewUnits, 0, p.use_many ? kFewRows : INT_MAX};
+    p.many = {kManyTile, kManyUnits, p.use_few ? kFewRows : 0, INT_MAX};
+    const bool join = max_pages > kLeastPages;   // otherwise a tile is one piece
+    if (p.use_few) {
+        const int rows = p.use_many ? std::min(max_rows, std::max(1, kFewRows / (Hq / Hk))) : max_rows;
+        p.few_pieces = most_pieces(p.few, S, T, rows, Hq, Hk, max_pages);
+        p.few_tiles = most_tiles(p.few, S, T, rows, Hq, Hk);
+        p.few_bytes = join ? (size_t)p.few_pieces * kFewTile * (d + 2) * sizeof(float) : 0;
+    }
+    if (p.use_many) {
+        p.many_pieces = (most_pieces(p.many, S, T, max_rows, Hq, Hk, max_pages) + 7) / 8 * 8;
+        p.many_tiles = most_tiles(p.many, S, T, max_rows, Hq, Hk);
+        p.many_bytes = join ? (size_t)p.many_pieces * kManyTile * (d + 2) * sizeof(float) : 0;
+    }
+    return p;
 }
 
 }  // namespace
 
 size_t cache_attn_workspace_bytes(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages) {
-    if (max_pages <= kLeastPages) return 0;   // a piece a tile
-    return (size_t)most_pieces(S, T, max_rows, Hq, Hk, max_pages) * kTile * (d + 2) * sizeof(float);
+    const Plan p = make_plan(S, T, max_rows, Hq, Hk, d, max_pages);
+    return p.few_bytes + p.many_bytes;
+}
+
+template <int D, bool F32T, bool VEC>
+static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) {
+    const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)a.d));
+    float* many_ws = a.ws ? reinterpret_cast<float*>(static_cast<char*>(a.ws) + p.few_bytes) : nullptr;
+    hipError_t e = hipSuccess;
+    if (p.use_many) {
+        cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 256, 0, st>>>(a, p.many, scale_log2, many_ws);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (p.use_few) {
+        cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_pieces, 64, 0, st>>>(a, p.few, scale_log2);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (p.many_bytes) {
+        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.many_tiles, kManyTile / 16), 256, 0, st>>>(a, p.many, (unsigned)p.many_pieces, many_ws);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (p.few_bytes) {
+        cache_join_kernel<D, F32T, VEC><<<(unsigned)p.few_tiles, 256, 0, st>>>(a, p.few, (unsigned)p.few_pieces, static_cast<const float*>(a.ws));
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t st) {
     const int size = a.dtype == 0 ? 2 : 4;
     const bool vec = ((reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.out)) & 15) == 0 &&
                      ((a.sq.h | a.sq.n | a.so.h | a.so.n) * size & 15) == 0;
-    const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)a.d));
-    const unsigned grid = (unsigned)most_pieces(a.S, a.T, a.max_rows, a.Hq, a.Hk, a.max_pages);
-    const unsigned tiles = (unsigned)most_tiles(a.S, a.T, a.max_rows, a.Hq, a.Hk);
-    const bool join = a.max_pages > kLeastPages;
-#define SOL_ATTN(D, F)                                                                         \
-    do {                                                                                       \
-        if (vec) cache_attn_kernel<D, F, true><<<grid, 64, 0, st>>>(a, scale_log2);            \
-        else cache_attn_kernel<D, F, false><<<grid, 64, 0, st>>>(a, scale_log2);               \
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;                       \
-        if (join) cache_join_kernel<D, F><<<tiles, 256, 0, st>>>(a, grid);                           \
-    } while (0)
+    const Plan p = make_plan(a.S, a.T, a.max_rows, a.Hq, a.Hk, a.d, a.max_pages);
     if (a.dtype == 0) {
-        if (a.d == 128) SOL_ATTN(128, false);
-        else SOL_ATTN(64, false);
-    } else {
-        if (a.d == 128) SOL_ATTN(128, true);
-        else SOL_ATTN(64, true);
+        if (a.d == 128) return vec ? launch<128, false, true>(a, p, st) : launch<128, false, false>(a, p, st);
+        return vec ? launch<64, false, true>(a, p, st) : launch<64, false, false>(a, p, st);
     }
-#undef SOL_ATTN
-    return hipGetLastError();
+    if (a.d == 128) return vec ? launch<128, true, true>(a, p, st) : launch<128, true, false>(a, p, st);
+    return vec ? launch<64, true, true>(a, p, st) : launch<64, true, false>(a, p, st);
 }
 
 }  // namespace sol

@@ -19,7 +19,7 @@ INVALID, UNSUPPORTED, WORKSPACE = sb.SOL_ERR_INVALID_ARG, sb.SOL_ERR_UNSUPPORTED
 
 
 def strides(*s):
-    return ctypes.cast((ctypes.c_longlong * len(s))(*s), P)
+    return (ctypes.c_longlong * len(s))(*s)
 
 
 def test_library_exports_every_declared_symbol():
