@@ -19,6 +19,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 namespace sol {
 namespace {
@@ -339,12 +340,27 @@ struct FewPage {
     uint32_t ks;           // byte 2 b + w
 };
 
+// A lane's byte offsets inside a page: the page itself is a scalar address.
+struct FewOffsets {
+    uint32_t k, ks, v, vs;
+};
+
 template <int D>
-__device__ __forceinline__ void few_load_k(const uint8_t* page, FewPage<D>& r) {
+__device__ __forceinline__ FewOffsets few_offsets() {
     using L = PageLayout<D>;
-    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-    const int key = 8 * (i >> 2) + (i & 3);
-    if (D == 64 && g >= 2) {
+    const unsigned lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    FewOffsets o;
+    o.k = L::k + (8 * (i >> 2) + (i & 3)) * (D / 2) + 16 * g;
+    // scale of (key, group g) at [g & 1][key with bits 2 and 3 exchanged][g >> 1][w]
+    o.ks = L::ks + ((g & 1) * 32 + 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3)) * (D / 32) + (g >> 1) * 2;
+    o.v = L::v + (g * 32 + 2 * i) * (D / 8);
+    o.vs = L::vs + (g * (D / 32) + i / (512 / D)) * 8;
+    return o;
+}
+
+template <int D>
+__device__ __forceinline__ void few_load_k(const uint8_t* page, const FewOffsets& at, FewPage<D>& r) {
+    if (D == 64 && (threadIdx.x & 32)) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) r.k[t] = u32x4{0, 0, 0, 0};
         r.ks = 0x7f7f7f7fu;
@@ -352,23 +368,18 @@ __device__ __forceinline__ void few_load_k(const uint8_t* page, FewPage<D>& r) {
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t)
-        r.k[t] = *reinterpret_cast<const u32x4*>(page + L::k + (32 * (t >> 1) + key + 4 * (t & 1)) * (D / 2) + 16 * g);
-    // scale of (key, group g) at [g & 1][key with bits 2 and 3 exchanged][g >> 1][w]
-    const int at = ((g & 1) * 32 + 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3)) * (D / 32) + (g >> 1) * 2;
-    r.ks = *reinterpret_cast<const uint16_t*>(page + L::ks + at) |
-           ((uint32_t)*reinterpret_cast<const uint16_t*>(page + L::ks + at + 8 * (D / 32)) << 16);
+        r.k[t] = *reinterpret_cast<const u32x4*>(page + (32 * (t >> 1) + 4 * (t & 1)) * (D / 2) + at.k);
+    r.ks = *reinterpret_cast<const uint16_t*>(page + at.ks) | ((uint32_t)*reinterpret_cast<const uint16_t*>(page + 8 * (D / 32) + at.ks) << 16);
 }
 
 template <int D>
-__device__ __forceinline__ void few_load_v(const uint8_t* page, FewPage<D>& r) {
-    using L = PageLayout<D>;
-    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void few_load_v(const uint8_t* page, const FewOffsets& at, FewPage<D>& r) {
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
 #pragma unroll
         for (int c = 0; c < D / 64; ++c)   // 32 bytes (d = 64: 16) of two channel runs
-            r.v[w][c] = *reinterpret_cast<const u32x4*>(page + L::v + ((4 * w + g) * 32 + 2 * i) * (D / 8) + 16 * c);
-        r.vs[w] = *reinterpret_cast<const u32x2*>(page + L::vs + ((4 * w + g) * (D / 32) + i / (512 / D)) * 8);
+            r.v[w][c] = *reinterpret_cast<const u32x4*>(page + w * 128 * (D / 8) + 16 * c + at.v);
+        r.vs[w] = *reinterpret_cast<const u32x2*>(page + w * (D / 8) * 8 + at.vs);
     }
 }
 
@@ -499,29 +510,30 @@ __global__ __launch_bounds__(64, F32T ? 2 : 3) void cache_few_kernel(const Cache
     for (int t = 0; t < CT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = kLowest, l = 0.f;
     FewPage<D> pg;
+    const FewOffsets at = few_offsets<D>();
     int p = pc.p0, id = 0;
     bool more = next_page(table, a.P, p1, p, id);
     const uint8_t* page = store + id * page_stride;
     if (more) {
-        few_load_k<D>(page, pg);
-        few_load_v<D>(page, pg);
+        few_load_k<D>(page, at, pg);
+        few_load_v<D>(page, at, pg);
     }
     const Split<NT> q = split_row<NT>(x);
-    while (more) {
+    auto step = [&](auto edge) __attribute__((always_inline)) {
+        constexpr bool EDGE = decltype(edge)::value;
         const int key0 = p * kPage;
         ++p;
         more = next_page(table, a.P, p1, p, id);
-        const bool edge = key0 + kPage > least;
-        if (edge) few_first<D, F32T, true>(pg, q, key0, sees, s);
-        else few_first<D, F32T, false>(pg, q, key0, sees, s);
+        few_first<D, F32T, EDGE>(pg, q, key0, sees, s);
         if (more) {
             page = store + id * page_stride;
-            few_load_k<D>(page, pg);
+            few_load_k<D>(page, at, pg);
         }
-        if (edge) few_second<D, F32T, true>(pg, s, key0, most, scale_log2, m, l, o);
-        else few_second<D, F32T, false>(pg, s, key0, most, scale_log2, m, l, o);
-        if (more) few_load_v<D>(page, pg);
-    }
+        few_second<D, F32T, EDGE>(pg, s, key0, most, scale_log2, m, l, o);
+        if (more) few_load_v<D>(page, at, pg);
+    };
+    while (more && p * kPage + kPage <= least) step(std::false_type{});
+    while (more) step(std::true_type{});
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (!valid) return;
