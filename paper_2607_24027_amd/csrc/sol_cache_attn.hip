@@ -36,10 +36,12 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
 constexpr int kFewRows = 48;                    // a request of more goes to cache_many_kernel
-constexpr int kFewUnits = 3072;                 // pieces that a launch aims at: 12 waves a compute unit
-constexpr int kManyUnits = 1024;                // two workgroups a compute unit, twice
+constexpr int kFewSlots = 3072;                 // waves of cache_few_kernel that the GPU holds, 12 a compute unit
+constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit
+constexpr int kRounds = 7;                      // fillings of those slots at most
+constexpr int kFewCost = 2, kManyCost = 8;      // what starting a piece and joining its result costs, in pages
 constexpr int kLeastPages = 2;                  // least pages of a piece
-constexpr int kSlackPieces = 64;                // the mean number of pages is formed in f32
+constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
 constexpr float kShift = 7.0f;   // probabilities are held as 2^7 p: f16 keeps all bits down to 2^-21 of the maximum's
 constexpr float kSlack = 8.0f;   // log2 by which a logit may pass the running maximum before it is raised (2^15 < 65504)
 constexpr float kLowest = -3.402823466e38f;
@@ -59,7 +61,7 @@ struct Request {
 
 // Requests with rows in (LO, HI] take part.
 struct Part {
-    int tile, units, lo, hi;
+    int tile, slots, cost, lo, hi;
 };
 
 __device__ __forceinline__ Request request(const CacheAttnArgs& a, const Part& part, int s, int G) {
@@ -95,20 +97,55 @@ __device__ __forceinline__ T at_lane(T x, int lane) {
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
 }
 
-// Every tile of every request is cut into pieces of about the same number of pages: `units` pieces in all, and one more a tile
-// at most.  Piece `id` (BY_TILE: share 0 of tile `id`); false past the last.  Pieces go by request, head, share, tile.  By the
-// lanes of one wave, on values that all waves of the launch and of the join see alike.
+// Largest value of a wave's lanes.
+__device__ __forceinline__ int wave_max(int x) {
+#define SOL_STEP(ctrl, rows) x = max(x, __builtin_amdgcn_update_dpp(x, x, ctrl, rows, 0xf, false))
+    SOL_STEP(0x111, 0xf);
+    SOL_STEP(0x112, 0xf);
+    SOL_STEP(0x114, 0xf);
+    SOL_STEP(0x118, 0xf);
+    SOL_STEP(0x142, 0xa);
+    SOL_STEP(0x143, 0xc);
+#undef SOL_STEP
+    return at_lane(x, 63);
+}
+
+// Pages of a piece, at most, by which `tiles` tiles of `pages` pages in all become no more pieces than fill the slots k times.
+__device__ __forceinline__ int pages_for(float pages, unsigned tiles, int slots, int k) {
+    const float room = (float)slots * (float)k - (float)tiles;   // each tile rounds up by one piece at most
+    return room < 1.f ? 1 << 30 : (int)fmaxf(ceilf(pages / room), (float)kLeastPages);
+}
+
+// Every tile of every request is cut into equal pieces of at most `per` pages.  With few tiles, the pieces fill the slots once; otherwise
+// `per` is chosen among fillings of one to kRounds times by the rounds that the pieces take and the longest piece.  Past 64
+// requests (a second load for each lane) it is two fillings, or no cut at all.
+//
+// Piece `id` (BY_TILE: share 0 of tile `id`); false past the last.  Pieces go by request, head, share, tile.  By the lanes of
+// one wave, on values that all waves of the launch and of the join see alike.
 template <bool BY_TILE>
 __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& part, unsigned id, bool spread, Piece& out) {
     const int lane = threadIdx.x & 63, G = a.Hq / a.Hk;
     float sum = 0.f;
+    unsigned tiles = 0;
     Request r = {};
     for (int s = lane; s < a.S; s += 64) {
         r = request(a, part, s, G);   // of up to 64 requests, each lane's own
         sum += (float)r.tiles * (float)r.pages;
+        tiles += (unsigned)r.tiles;
     }
-    const float all = at_lane(scan_add(sum), 63);
-    const int per = (int)fmaxf(ceilf(all * (float)a.Hk / (float)part.units), (float)kLeastPages);
+    sum = at_lane(scan_add(sum), 63) * (float)a.Hk;
+    tiles = at_lane(scan_add(tiles), 63) * a.Hk;
+    int per = pages_for(sum, tiles, part.slots, a.S > 64 ? 2 : 1);
+    if (a.S <= 64 && tiles > (unsigned)part.slots / 2) {
+        float least = INFINITY;
+        for (int k = 1; k <= kRounds; ++k) {
+            const int p = pages_for(sum, tiles, part.slots, k), chunks = (r.pages + p - 1) / p;
+            const unsigned pieces = at_lane(scan_add((unsigned)(r.tiles * chunks)), 63) * a.Hk;
+            const int longest = wave_max(r.tiles ? (r.pages + chunks - 1) / chunks : 0);
+            const float cost = (float)((pieces + part.slots - 1) / part.slots) * (float)(longest + part.cost);
+            if (cost < least) least = cost, per = p;
+        }
+    }
     if (spread) {
         // neighbouring workgroups run on different dies: give each die a run of neighbouring pieces, which share keys
         unsigned total = 0;
@@ -140,13 +177,13 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& p
             out.tiles = at_lane(r.tiles, l);
             const int pages = at_lane(r.pages, l);
             out.chunks = at_lane(chunks, l);
-            const unsigned tiles = out.tiles, each = BY_TILE ? tiles : tiles * out.chunks;
+            const unsigned each = BY_TILE ? out.tiles : out.tiles * out.chunks;
             if (each == 0) return false;
             out.hk = (int)(within / each);
             const unsigned rest = within % each;
-            out.chunk = (int)(rest / tiles);
-            out.tile = (int)(rest % tiles);
-            out.slot0 = slots + at_lane(slot_upto - pieces, l) + (unsigned)out.hk * tiles * out.chunks + out.tile;
+            out.chunk = (int)(rest / (unsigned)out.tiles);
+            out.tile = (int)(rest % (unsigned)out.tiles);
+            out.slot0 = slots + at_lane(slot_upto - pieces, l) + (unsigned)(out.hk * out.tiles * out.chunks + out.tile);
             // equal shares of the pages
             out.p0 = (int)((long long)pages * out.chunk / out.chunks);
             out.p1 = (int)((long long)pages * (out.chunk + 1) / out.chunks);
@@ -156,6 +193,24 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& p
         slots += at_lane(slot_upto, 63);
     }
     return false;
+}
+
+// find_piece() by the first wave of a workgroup, for all.
+template <bool BY_TILE>
+__device__ __forceinline__ bool find_piece_shared(const CacheAttnArgs& a, const Part& part, unsigned id, bool spread, Piece& out) {
+    __shared__ Piece s_piece;
+    __shared__ int s_found;
+    if (threadIdx.x < 64) {
+        const bool found = find_piece<BY_TILE>(a, part, id, spread, out);
+        if (threadIdx.x == 0) s_piece = out, s_found = found;
+    }
+    __syncthreads();
+    int w[sizeof(Piece) / 4];
+    __builtin_memcpy(w, &s_piece, sizeof w);
+#pragma unroll
+    for (int& x : w) x = __builtin_amdgcn_readfirstlane(x);
+    __builtin_memcpy(&out, w, sizeof w);
+    return __builtin_amdgcn_readfirstlane(s_found);
 }
 
 // ---------------------------------------------------------------------------
@@ -473,7 +528,7 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64, F32T ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2) {
+__global__ __launch_bounds__(64, 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, CT = D / 16;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
@@ -709,7 +764,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece<false>(a, part, blockIdx.x, true, pc)) return;   // alike in the four waves
+    if (!find_piece_shared<false>(a, part, blockIdx.x, true, pc)) return;
     const unsigned slot = pc.slot0 + (unsigned)pc.chunk * pc.tiles;
 
     const int r = pc.tile * kManyTile + 32 * wave + j;
@@ -801,28 +856,30 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
 }
 
 // ---------------------------------------------------------------------------
-// Joins the shares of 16 rows of a tile in their order.  D / 4 threads a row and group of shares, four channels each: with few
-// rows the shares are dealt to several groups, whose sums are added in LDS.
+// Joins the shares of a tile's rows, four rows at a time, in an order that the plan fixes.  D / 4 threads hold a row, four channels
+// each; the shares are dealt to several such groups, whose sums are added in LDS.
 // ---------------------------------------------------------------------------
+constexpr int kJoinRows = 4, kJoinThreads = 512;
+
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a, const Part part, const unsigned pieces, const float* ws) {
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttnArgs a, const Part part, const unsigned pieces, const float* ws) {
+    constexpr int LANES = D / 4, GROUPS = kJoinThreads / LANES;
     __shared__ f32x4 s_o[GROUPS][LANES];
     __shared__ float s_l[GROUPS];
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece<true>(a, part, blockIdx.x, false, pc) || pc.chunks == 1) return;
+    if (!find_piece_shared<true>(a, part, blockIdx.x, false, pc) || pc.chunks == 1) return;
     if (pc.slot0 + (uint64_t)(pc.chunks - 1) * pc.tiles >= pieces) return;   // rows that overlap: no room was asked for
-    const int first = pc.tile * part.tile + 16 * blockIdx.y, rows = min(pc.rows - first, 16);
-    if (rows <= 0) return;
     const long long stride = (long long)pc.tiles * (part.tile * (D + 2));
-    const float* at = ws + (long long)pc.slot0 * (part.tile * (D + 2)) + 2 * 16 * blockIdx.y;   // (max, sum) pairs of the rows
-    const float* ot = ws + (long long)pc.slot0 * (part.tile * (D + 2)) + 2 * part.tile + 16 * blockIdx.y * D;
+    const float* const tile = ws + (long long)pc.slot0 * (part.tile * (D + 2));
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    // rows at a time: a power of two, so that the groups of a row are equally many
-    const int width = rows == 1 ? 1 : rows == 2 ? 2 : rows <= 4 ? 4 : min(GROUPS, 8), shares = GROUPS / width;
-    for (int j0 = 0; j0 < rows; j0 += width) {
-        const int j = j0 + group % width, share = group / width;
+    for (int row0 = kJoinRows * blockIdx.y; row0 < part.tile; row0 += kJoinRows * gridDim.y) {
+        const int first = pc.tile * part.tile + row0, rows = min(pc.rows - first, kJoinRows);
+        if (rows <= 0) return;
+        const float* at = tile + 2 * row0;   // (max, sum) pairs of the rows
+        const float* ot = tile + 2 * part.tile + row0 * D;
+        const int width = rows <= 2 ? rows : kJoinRows, shares = GROUPS / width;
+        const int j = group % width, share = group / width;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
         float l = 0.f;
         if (j < rows) {
@@ -837,19 +894,16 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a, 
                 o += w * *reinterpret_cast<const f32x4*>(ot + c * stride + j * D + 4 * lane);
             }
         }
-        if (shares > 1) {
-            __syncthreads();
-            s_o[group][lane] = o;
-            if (lane == 0) s_l[group] = l;
-            __syncthreads();
-            if (share == 0)
-                for (int x = 1; x < shares; ++x) o += s_o[group + x * width][lane], l += s_l[group + x * width];
-        }
-        if (j < rows && share == 0) {
+        s_o[group][lane] = o;
+        if (lane == 0) s_l[group] = l;
+        __syncthreads();
+        if (share == 0 && j < rows) {
+            for (int x = 1; x < min(shares, pc.chunks); ++x) o += s_o[j + x * width][lane], l += s_l[j + x * width];
             const float inv = l == 0.f ? 0.f : 1.0f / l;
             const int r = first + j;
             store_run<F32T, VEC>(a.out, (pc.hk * G + r % G) * a.so.h + (pc.row0 + r / G) * a.so.n + 4 * lane, o * inv, 4);
         }
+        __syncthreads();
     }
 }
 
@@ -862,10 +916,12 @@ long long most_tiles(const Part& part, int S, int T, int max_rows, int Hq, int H
     return (rows / part.tile + requests) * Hk;
 }
 
-// Pieces at most: a piece's pages are rounded up, so a tile adds one to `units`; and no tile has more than its pages give.
+// Pieces at most: what fills the slots kRounds times, or one for each tile; and no tile has more than its pages give.
 long long most_pieces(const Part& part, int S, int T, int max_rows, int Hq, int Hk, int max_pages) {
     const long long tiles = most_tiles(part, S, T, max_rows, Hq, Hk);
-    return std::min(tiles + part.units + kSlackPieces, tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
+    // up to half the slots in tiles become one filling, more of them up to kRounds
+    const long long rounds = tiles > part.slots / 2 || S > 64 ? kRounds : 1;
+    return std::min(std::max(tiles, rounds * part.slots + kSlackPieces), tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
 }
 
 struct Plan {
@@ -882,8 +938,8 @@ Plan make_plan(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages)
     const long long most = (long long)std::min(max_rows, T) * (Hq / Hk);
     p.use_many = most > kFewRows;
     p.use_few = !p.use_many || S > 1;
-    p.few = {kFewTile, kFewUnits, 0, p.use_many ? kFewRows : INT_MAX};
-    p.many = {kManyTile, kManyUnits, p.use_few ? kFewRows : 0, INT_MAX};
+    p.few = {kFewTile, kFewSlots, kFewCost, 0, p.use_many ? kFewRows : INT_MAX};
+    p.many = {kManyTile, kManySlots, kManyCost, p.use_few ? kFewRows : 0, INT_MAX};
     const bool join = max_pages > kLeastPages;   // otherwise a tile is one piece
     if (p.use_few) {
         const int rows = p.use_many ? std::min(max_rows, std::max(1, kFewRows / (Hq / Hk))) : max_rows;
@@ -920,11 +976,11 @@ static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) 
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.many_bytes) {
-        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.many_tiles, kManyTile / 16), 256, 0, st>>>(a, p.many, (unsigned)p.many_pieces, many_ws);
+        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.many_tiles, kManyTile / 32), kJoinThreads, 0, st>>>(a, p.many, (unsigned)p.many_pieces, many_ws);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.few_bytes) {
-        cache_join_kernel<D, F32T, VEC><<<(unsigned)p.few_tiles, 256, 0, st>>>(a, p.few, (unsigned)p.few_pieces, static_cast<const float*>(a.ws));
+        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.few_tiles, kFewTile / kJoinRows), kJoinThreads, 0, st>>>(a, p.few, (unsigned)p.few_pieces, static_cast<const float*>(a.ws));
         e = hipGetLastError();
     }
     return e;
