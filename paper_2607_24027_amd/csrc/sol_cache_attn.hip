@@ -352,16 +352,16 @@ __device__ __forceinline__ void scales_of(u32x2 b, float (&scale)[8]) {
     }
 }
 
-// Probabilities as f16 operands: cut to f16 (F32T: two terms), and their sum as cut added to l.
+// Probabilities as f16 operands, rounded to nearest (F32T: two terms), and their sum, in f32, added to l.  (A sum of the rounded ones by
+// v_dot2_f32_f16 takes half the instructions, but they do not run beside those of the matrix cores.)
 template <bool F32T>
 __device__ __forceinline__ void cut_pair(float e0, float e1, f16x8& hi, f16x8& lo, int i, float& l) {
-    const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e0, e1));
+    const f16x2 h = {(_Float16)e0, (_Float16)e1};
     hi[2 * i] = h[0], hi[2 * i + 1] = h[1];
-    l = __builtin_amdgcn_fdot2(h, f16x2{1, 1}, l, false);
+    l += e0;
+    l += e1;
     if constexpr (F32T) {
-        const f16x2 r = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e0 - (float)h[0], e1 - (float)h[1]));
-        lo[2 * i] = r[0], lo[2 * i + 1] = r[1];
-        l = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l, false);
+        lo[2 * i] = (_Float16)(e0 - (float)h[0]), lo[2 * i + 1] = (_Float16)(e1 - (float)h[1]);
     }
 }
 
@@ -715,7 +715,8 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
     }
     // register 8u + 4b + e of window w is key 32w + 16u + 8h + 4b + e
     if (edge) {
-        const int left = sees - key0 - 8 * h;
+        int left = sees - key0 - 8 * h;
+        asm volatile("" : "+v"(left));   // a branch, not an instruction more for every logit of every page
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
