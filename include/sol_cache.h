@@ -145,10 +145,9 @@ int sol_cache_read(const void* store, const int32_t* slots, void* k_out, void* v
  * workspace: device scratch of at least sol_cache_workspace_bytes(...) bytes that starts on 16 bytes; calls that
  *   may run at the same time need different ones, and a captured graph keeps using the one
  *   it was captured with.  It may be NULL where 0 bytes are needed.
- * Logits, maxima and sums are f32.  bf16: q is split into three 6-bit floats for each channel, whose
- *   sum differs from it by at most 2^-13 of the largest magnitude of its 32 channels, and not at all
- *   where it is above 1/60 of that; probabilities are cut to f16 and summed as cut.  f32: six such
- *   terms (2^-24), probabilities in two f16 terms.
+ * Logits, maxima and sums are f32.  q log2(e) / sqrt(d) is split into 6-bit floats for each channel: three (bf16), whose
+ *   sum is off by at most 2^-12.9 of the largest magnitude of its 32 channels, or six (f32, 2^-24.9).  Probabilities are
+ *   rounded to f16, in f32 to two such terms; their sum is taken before.
  * Results do not depend on the order in which the GPU runs the work.
  */
 int sol_cache_forward(const void* q, const long long* q_strides, void* out, const long long* out_strides,

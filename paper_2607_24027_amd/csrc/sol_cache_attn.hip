@@ -4,10 +4,11 @@
 // row is a (token, query head of the group) pair of one key/value head.
 //
 //   q . k   v_mfma_scale_f32_*_f8f6f4 takes the codes of the cache as they lie in memory, with their scales.  Its other operand
-//           holds q as a sum of 6-bit floats (e2m3, four significant bits each, every term at a sixteenth of the scale of the one
-//           before): three terms for bf16, which has eight significant bits, six for f32.  6-bit operands run at twice the
-//           rate of 8-bit ones (32 against 64 cycles for 32 x 32 x 64), and sums of their products lose nothing, where those
-//           of 8-bit floats, whose exponents reach further, were off by 2^-15 of the largest product.
+//           holds q log2(e) / sqrt(d) as a sum of 6-bit floats (e2m3, four significant bits each, every term at a sixteenth of
+//           the scale of the one before): three terms for bf16, six for f32.  6-bit operands run at twice the rate of 8-bit
+//           ones (32 against 64 cycles for 32 x 32 x 64), and sums of their products lose nothing, where those of 8-bit
+//           floats, whose exponents reach further, were off by 2^-15 of the largest product.  The accumulators start at
+//           7 - m, m the running maximum: what comes out is the exponent of 2^7 p, and nothing is left to do but exp2.
 //   p . v   values are converted to f16 (exact), probabilities to f16 too: v_mfma_f32_*_f16.
 //
 // Two kernels.  Requests of few rows: a wave takes 16 rows and a share of the keys, bytes of the cache go from memory to
@@ -43,7 +44,7 @@ constexpr int kFewCost = 2, kManyCost = 8;      // what starting a piece and joi
 constexpr int kLeastPages = 2;                  // least pages of a piece
 constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
 constexpr float kShift = 7.0f;   // probabilities are held as 2^7 p: f16 keeps all bits down to 2^-21 of the maximum's
-constexpr float kSlack = 8.0f;   // log2 by which a logit may pass the running maximum before it is raised (2^15 < 65504)
+constexpr float kMost = 15.0f;   // exponent past which the running maximum is raised: 2^15 < 65504
 constexpr float kLowest = -3.402823466e38f;
 
 // The piece of work of one workgroup.
@@ -370,14 +371,43 @@ __device__ __forceinline__ int row_limit(const CacheAttnArgs& a, int token, int 
     return pos < 0 ? 0 : (int)min(((long long)pos / a.granule + 1) * a.granule, (long long)len);
 }
 
-// The next page that is there, from p on.
-__device__ __forceinline__ bool next_page(const int* table, int P, int p1, int& p, int& id) {
-    while (p < p1) {
-        id = table[p];
-        if (id >= 0 && id < P) return true;
-        ++p;
+// The pages of a piece in order, those that are not there left out.  A lane holds the table entry of one of 64 pages.
+struct Pages {
+    const int* table;
+    int P, end, base;    // pages base ... base + 63 are in `entry`
+    uint64_t there;      // those of them that are there and not yet given out
+    int entry, p;        // p: the page that next() found
+
+    __device__ __forceinline__ void fill() {
+        const int at = base + (int)(threadIdx.x & 63);
+        entry = at < end ? table[at] : -1;
+        there = __ballot(entry >= 0 && entry < P);
     }
-    return false;
+    __device__ __forceinline__ Pages(const int* t, int P_, int p0, int p1) : table(t), P(P_), end(p1), base(p0), there(0), entry(-1), p(p0) { fill(); }
+    // The next page's place in the store, or -1.
+    __device__ __forceinline__ int next() {
+        while (!there) {
+            base += 64;
+            if (base >= end) return -1;
+            fill();
+        }
+        const int l = __builtin_ctzll(there);
+        there &= there - 1;
+        p = base + l;
+        return __builtin_amdgcn_readlane(entry, l);
+    }
+};
+
+// Raises the running maximum of a lane's row (exponents s, sums l and o) to `top`, the row's largest exponent, where that is past
+// `most`: -infinity before the row has seen a key, kMost afterwards.  For a wave in which one row's is; returns the change.
+__device__ __forceinline__ float raise(float top, float& m, float& most, float& alpha) {
+    const bool fresh = most < 0.f;
+    float by = fresh ? top - kShift : fmaxf(top - kShift, 0.f);
+    if (top == -INFINITY) by = 0.f;
+    else most = kMost;
+    alpha = fresh ? 0.f : __builtin_amdgcn_exp2f(-by);
+    m += by;
+    return by;
 }
 
 // ---------------------------------------------------------------------------
@@ -439,11 +469,11 @@ __device__ __forceinline__ void few_load_v(const uint8_t* page, const FewOffsets
 }
 
 template <int D, bool F32T, bool EDGE>
-__device__ __forceinline__ void few_first(const FewPage<D>& pg, const Split<F32T ? 6 : 3>& q, int key0, int sees, f32x4 (&s)[4]) {
+__device__ __forceinline__ void few_first(const FewPage<D>& pg, const Split<F32T ? 6 : 3>& q, int key0, int sees, float off, f32x4 (&s)[4]) {
     constexpr int NT = F32T ? 6 : 3;
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 4; ++t) s[t] = f32x4{off, off, off, off};
 #define SOL_MFMA(t, ks_byte, n, q_byte)                                                                                   \
     s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i32x8{(int)pg.k[t][0], (int)pg.k[t][1], (int)pg.k[t][2], (int)pg.k[t][3], 0, 0, 0, 0},   \
                                                             i32x8{(int)q.w[n][0], (int)q.w[n][1], (int)q.w[n][2], (int)q.w[n][3], (int)q.w[n][4], (int)q.w[n][5], 0, 0}, \
@@ -470,7 +500,7 @@ __device__ __forceinline__ void few_first(const FewPage<D>& pg, const Split<F32T
 }
 
 template <int D, bool F32T, bool EDGE>
-__device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], int key0, int most, float scale_log2, float& m, float& l,
+__device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], int key0, int last, float& m, float& most, float& l,
                                            f32x4 (&o)[D / 16]) {
     const int g = (threadIdx.x & 63) >> 4;
     float top = s[0][0];
@@ -478,18 +508,17 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
-    top *= scale_log2;
-    // lanes of a row that lags behind see it in their own part first: the vote is over all of them
-    if (__any(top > m + kSlack)) {
+    if (__any(top > most)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float up = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - up);
-        m = up;
+        float alpha;
+        const float by = raise(top, m, most, alpha);
         l *= alpha;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t] -= by;
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
     }
-    const float off = kShift - m;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
         f16x8 ph = {}, pl = {};
@@ -497,14 +526,13 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                cut_pair<F32T>(__builtin_amdgcn_exp2f(fmaf(s[2 * w + b][2 * e], scale_log2, off)),
-                               __builtin_amdgcn_exp2f(fmaf(s[2 * w + b][2 * e + 1], scale_log2, off)), ph, pl, 2 * b + e, l);
+                cut_pair<F32T>(__builtin_amdgcn_exp2f(s[2 * w + b][2 * e]), __builtin_amdgcn_exp2f(s[2 * w + b][2 * e + 1]), ph, pl, 2 * b + e, l);
         float vs[8];
         scales_of(pg.vs[w], vs);
         if constexpr (EDGE) {   // what lies behind the last token may be anything: a finite scale keeps 0 v = 0
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (key0 + 32 * w + 8 * g + i >= most) vs[i] = 1.0f;
+                if (key0 + 32 * w + 8 * g + i >= last) vs[i] = 1.0f;
         }
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
@@ -528,7 +556,7 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64, 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2) {
+__global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, CT = D / 16;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
@@ -547,48 +575,47 @@ __global__ __launch_bounds__(64, 3) void cache_few_kernel(const CacheAttnArgs a,
 #pragma unroll
         for (int i = 0; i < 32; ++i) x[i] = 0.f;
     }
-    int most = sees, least = sees;
+    int last = sees, least = sees;
 #pragma unroll
     for (int m = 1; m < 16; m *= 2) {
-        most = max(most, __shfl_xor(most, m));
+        last = max(last, __shfl_xor(last, m));
         least = min(least, __shfl_xor(least, m));
     }
-    most = __builtin_amdgcn_readfirstlane(most);
+    last = __builtin_amdgcn_readfirstlane(last);
     least = __builtin_amdgcn_readfirstlane(least);
-    const int p1 = min(pc.p1, (most + kPage - 1) / kPage);
-    const int* table = a.table + (long long)pc.s * a.max_pages;
+    Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, min(pc.p1, (last + kPage - 1) / kPage));
     const long long page_stride = (long long)a.Hk * L::bytes;
     const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
 
     f32x4 o[CT], s[4];
 #pragma unroll
     for (int t = 0; t < CT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = kLowest, l = 0.f;
+    float m = 0.f, most = -INFINITY, l = 0.f;
     FewPage<D> pg;
     const FewOffsets at = few_offsets<D>();
-    int p = pc.p0, id = 0;
-    bool more = next_page(table, a.P, p1, p, id);
+    int id = pages.next();
     const uint8_t* page = store + id * page_stride;
-    if (more) {
+    if (id >= 0) {
         few_load_k<D>(page, at, pg);
         few_load_v<D>(page, at, pg);
     }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] *= scale_log2;
     const Split<NT> q = split_row<NT>(x);
     auto step = [&](auto edge) __attribute__((always_inline)) {
         constexpr bool EDGE = decltype(edge)::value;
-        const int key0 = p * kPage;
-        ++p;
-        more = next_page(table, a.P, p1, p, id);
-        few_first<D, F32T, EDGE>(pg, q, key0, sees, s);
-        if (more) {
+        const int key0 = pages.p * kPage;
+        id = pages.next();
+        few_first<D, F32T, EDGE>(pg, q, key0, sees, kShift - m, s);
+        if (id >= 0) {
             page = store + id * page_stride;
             few_load_k<D>(page, at, pg);
         }
-        few_second<D, F32T, EDGE>(pg, s, key0, most, scale_log2, m, l, o);
-        if (more) few_load_v<D>(page, at, pg);
+        few_second<D, F32T, EDGE>(pg, s, key0, last, m, most, l, o);
+        if (id >= 0) few_load_v<D>(page, at, pg);
     };
-    while (more && p * kPage + kPage <= least) step(std::false_type{});
-    while (more) step(std::true_type{});
+    while (id >= 0 && pages.p * kPage + kPage <= least) step(std::false_type{});
+    while (id >= 0) step(std::true_type{});
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (!valid) return;
@@ -604,7 +631,7 @@ __global__ __launch_bounds__(64, 3) void cache_few_kernel(const CacheAttnArgs a,
         return;
     }
     float* to = static_cast<float*>(a.ws) + (long long)blockIdx.x * (kFewTile * (D + 2));
-    if (g == 0) to[2 * j] = m, to[2 * j + 1] = l;
+    if (g == 0) to[2 * j] = most < 0.f ? kLowest : m, to[2 * j + 1] = l;
     float* po = to + 2 * kFewTile + j * D;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -658,19 +685,19 @@ __device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D>& r) {
     }
 }
 
-// most: tokens from here on of the page may be anything.
+// left: tokens of the page that there are; what lies behind them may be anything, and a finite scale keeps 0 v = 0.
 template <int D>
-__device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, int most) {
+__device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, int left) {
     constexpr int CT = D / 32;
     const int t = threadIdx.x;
     if (D == 128 || t < 128) st.k[t] = r.k;
     if (t < 64) st.ks[t] = r.ks;
     float vs[8];
     scales_of(r.vs, vs);
-    if (most < kPage) {
+    if (left < kPage) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (8 * (t >> 5) + i >= most) vs[i] = 1.0f;
+            if (8 * (t >> 5) + i >= left) vs[i] = 1.0f;
     }
     f16x8 va[CT];
     values_f16<D / 64>(r.v, vs, va);
@@ -681,14 +708,10 @@ __device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, i
 
 template <int D, bool F32T>
 __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ? 6 : 3> (&q)[D / 64], int key0, bool edge, int sees,
-                                          float scale_log2, float& m, float& l, f32x16 (&o)[D / 32]) {
+                                          float& m, float& most, f32x16& off, float& l, f32x16 (&o)[D / 32]) {
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5;
-    f32x16 s[2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[w][i] = 0.f;
+    f32x16 s[2] = {off, off};
     const int ks = (int)st.ks[lane];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -728,25 +751,27 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
     for (int w = 0; w < 2; ++w)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[w][i]);
-    top *= scale_log2;
-    if (__any(top > m + kSlack)) {
+    if (__any(top > most)) {
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float up = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - up);
-        m = up;
+        float alpha;
+        const float by = raise(top, m, most, alpha);
         l *= alpha;
 #pragma unroll
-        for (int t = 0; t < CT; ++t)
+        for (int i = 0; i < 16; ++i) off[i] = kShift - m;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
+        for (int w = 0; w < 2; ++w) s[w] -= by;
+#pragma unroll
+        for (int t = 0; t < CT; ++t) o[t] *= alpha;
     }
-    const float off = kShift - m;
+    // a wave in this part goes first: its vector instructions fill the gaps of the other one's products
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         f16x8 ph = {}, pl = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            cut_pair<F32T>(__builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + 2 * i], scale_log2, off)),
-                           __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + 2 * i + 1], scale_log2, off)), ph, pl, i, l);
+            cut_pair<F32T>(__builtin_amdgcn_exp2f(s[u >> 1][8 * (u & 1) + 2 * i]), __builtin_amdgcn_exp2f(s[u >> 1][8 * (u & 1) + 2 * i + 1]),
+                           ph, pl, i, l);
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
             const f16x8 va = st.v[(u * CT + t) * 64 + lane];
@@ -754,6 +779,7 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
             if constexpr (F32T) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pl, o[t], 0, 0, 0);
         }
     }
+    __builtin_amdgcn_s_setprio(0);
 }
 
 template <int D, bool F32T, bool VEC>
@@ -761,7 +787,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
     __shared__ Stage<D> stage[2];
-    __shared__ int s_most[4];
+    __shared__ int s_last[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hk;
     Piece pc;
@@ -769,7 +795,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     const unsigned slot = pc.slot0 + (unsigned)pc.chunk * pc.tiles;
 
     const int r = pc.tile * kManyTile + 32 * wave + j;
-    const bool valid = r < pc.rows, busy = pc.tile * kManyTile + 32 * wave < pc.rows;
+    const bool valid = r < pc.rows;
     const int token = pc.row0 + (valid ? r / G : 0), head = pc.hk * G + (valid ? r % G : 0);
     int sees = row_limit(a, token, pc.len);
     if (!valid) sees = 0;
@@ -778,55 +804,55 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     for (int c = 0; c < NC; ++c) {
         float x[32];
         load_row<F32T, VEC>(a.q, head * a.sq.h + token * a.sq.n + 64 * c + 32 * h, x);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] *= scale_log2;
         q[c] = split_row<NT>(x);
     }
-    int most = sees, least = valid ? sees : INT_MAX;
+    int last = sees, least = valid ? sees : INT_MAX;
 #pragma unroll
     for (int m = 1; m < 32; m *= 2) {
-        most = max(most, __shfl_xor(most, m));
+        last = max(last, __shfl_xor(last, m));
         least = min(least, __shfl_xor(least, m));
     }
-    most = __builtin_amdgcn_readfirstlane(most);
+    last = __builtin_amdgcn_readfirstlane(last);   // 0 where the wave has no rows
     least = __builtin_amdgcn_readfirstlane(least);
-    if (lane == 0) s_most[wave] = most;
+    if (lane == 0) s_last[wave] = last;
     __syncthreads();
-    const int all = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
-    const int p1 = __builtin_amdgcn_readfirstlane(min(pc.p1, (all + kPage - 1) / kPage));
-    const int* table = a.table + (long long)pc.s * a.max_pages;
+    const int all = max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3]));
+    Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, __builtin_amdgcn_readfirstlane(min(pc.p1, (all + kPage - 1) / kPage)));
     const long long page_stride = (long long)a.Hk * L::bytes;
     const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
 
-    f32x16 o[CT];
+    f32x16 o[CT], off;
 #pragma unroll
     for (int t = 0; t < CT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    float m = kLowest, l = 0.f;
+    float m = 0.f, most = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) off[i] = kShift;
 
-    // page p is in stage[turn], page pn in registers
+    // the page of tokens key0 ... is in stage[turn], the one after it in registers
     ManyPage<D> pg;
-    int p = pc.p0, id = 0;
-    bool more = next_page(table, a.P, p1, p, id);
-    int pn = p, turn = 0;
+    int id = pages.next(), turn = 0, key0 = pages.p * kPage;
+    bool more = id >= 0;
     if (more) {
         many_load<D>(store + id * page_stride, pg);
-        many_store<D>(pg, stage[0], pc.len - p * kPage);
-        ++pn;
+        many_store<D>(pg, stage[0], pc.len - key0);
+        id = pages.next();
+        if (id >= 0) many_load<D>(store + id * page_stride, pg);
     }
-    bool more_n = more && next_page(table, a.P, p1, pn, id);
-    if (more_n) many_load<D>(store + id * page_stride, pg);
     __syncthreads();
     while (more) {
-        const int key0 = p * kPage;
-        p = pn;
-        more = more_n;
+        const int now = key0;
+        more = id >= 0;
         if (more) {
-            many_store<D>(pg, stage[turn ^ 1], pc.len - p * kPage);
-            ++pn;
-            more_n = next_page(table, a.P, p1, pn, id);
-            if (more_n) many_load<D>(store + id * page_stride, pg);
+            key0 = pages.p * kPage;
+            many_store<D>(pg, stage[turn ^ 1], pc.len - key0);
+            id = pages.next();
+            if (id >= 0) many_load<D>(store + id * page_stride, pg);
         }
-        if (busy && key0 < most) many_page<D, F32T>(stage[turn], q, key0, key0 + kPage > least, sees, scale_log2, m, l, o);
+        if (now < last) many_page<D, F32T>(stage[turn], q, now, now + kPage > least, sees, m, most, off, l, o);
         turn ^= 1;
         __syncthreads();
     }
@@ -848,7 +874,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     if (slot >= gridDim.x) return;   // rows that overlap: no room was asked for
     float* to = ws + (long long)slot * (kManyTile * (D + 2));
     const int row = 32 * wave + j;
-    if (h == 0) to[2 * row] = m, to[2 * row + 1] = l;
+    if (h == 0) to[2 * row] = most < 0.f ? kLowest : m, to[2 * row + 1] = l;
     float* po = to + 2 * kManyTile + row * D;
 #pragma unroll
     for (int i = 0; i < 16; ++i)

@@ -257,19 +257,20 @@ def tolerance(dtype, q, k, out, spread, reach):
     """Bound of the error of one row of outputs.  With ds the error of a logit, a probability is off by 2 ds of itself at most
     (ds is small), and an output by that times sum p |v - out|: weights that all change alike leave it as it is.
 
-    ds: the terms that q is split into leave 2^-13 of the largest of 32 channels where a channel is below 1/60 of that (bf16), or
-    2^-24 of it (f32); sums of d products in f32, 2^-24 a term, on sum |q k|; the argument of the exponential, 4 roundings
-    of a number below |s| + 16.  Probabilities are cut to f16: 2^-10 (bf16), or in two terms 2^-20 (f32), and below 2^-21 of the
-    largest to steps of 2^-31 of it.  Sums of probabilities times values: f32, at most one rounding for 16 keys and 64 more for
-    shares and their join, on sum p |v|.  The result: one rounding of its type, and a quotient."""
+    ds: q log2(e) / sqrt(d) is split into 6-bit floats.  With 32 channels scaled so that the largest magnitude lies in (3.75, 7.5],
+    what a term leaves is at most half its step of 1/4 for magnitudes up to 4, and the next term is taken of 16 times that: three
+    terms (bf16) leave 2^-3 / 16^2, six (f32) 2^-3 / 16^5, and the factor two roundings.  Sums of d products in f32, 2^-24 a
+    term, on sum |q k|; the accumulator starts at a number below |s| + 16, four roundings of that.  Probabilities are rounded to
+    f16, half a step of 2^-11, or in two terms 2^-22 (f32), and below 2^-21 of the largest to steps of 2^-31 of it; their sum is
+    taken before: an error on sum p |v|.  Sums of probabilities times values: f32, at most one rounding for 16 keys and 64
+    more for shares and their join, on sum p |v|.  The result: one rounding of its type, and a quotient."""
     d, L = q.shape[0], k.shape[0]
-    block = np.abs(q).reshape(-1, 32)
-    top = np.repeat(block.max(1), 32)
-    lost = np.where(np.abs(q) <= top / 60, top * 2.0 ** -13, 0.0) if dtype == "bf16" else top * 2.0 ** -24
+    top = np.repeat(np.abs(q).reshape(-1, 32).max(1), 32)
+    lost = top * (2.0 ** -11 if dtype == "bf16" else 2.0 ** -23) / 3.75 + 2 * 2.0 ** -24 * np.abs(q)
     s = np.abs(k) @ np.abs(q) / math.sqrt(d)
     ds = (np.abs(k) @ lost) / math.sqrt(d) + d * 2.0 ** -24 * s + 4 * 2.0 ** -24 * (s + 16)
-    cut = 2.0 ** -10 if dtype == "bf16" else 2.0 ** -20
-    return (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * np.abs(out) + (2 * ds.max() + cut) * spread + L * 2.0 ** -31 * (spread + np.abs(out)) \
+    cut = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22
+    return (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * np.abs(out) + 2 * ds.max() * spread + cut * reach + L * 2.0 ** -31 * (spread + reach) \
         + (L / 16 + 64) * 2.0 ** -24 * reach
 
 
