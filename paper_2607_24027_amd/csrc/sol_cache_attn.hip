@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <cstddef>
 #include <type_traits>
 
 namespace sol {
@@ -29,16 +30,18 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
+constexpr int kManyWaves = 4;                    // waves of a workgroup of cache_many_kernel, 32 query rows each
+constexpr int kFewTile = 16, kManyTile = 32 * kManyWaves;   // query rows of a piece
 constexpr int kFewRows = 48;                    // a request of more goes to cache_many_kernel
 constexpr int kFewSlots = 3072;                 // waves of cache_few_kernel that the GPU holds, 12 a compute unit
-constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit
+constexpr int kManySlots = 2048 / kManyWaves;                 // workgroups of cache_many_kernel that it holds, two a compute unit
 constexpr int kRounds = 7;                      // fillings of those slots at most
 constexpr int kFewCost = 2, kManyCost = 8;      // what starting a piece and joining its result costs, in pages
 constexpr int kLeastPages = 2;                  // least pages of a piece
@@ -98,9 +101,10 @@ __device__ __forceinline__ T at_lane(T x, int lane) {
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
 }
 
-// Largest value of a wave's lanes.
-__device__ __forceinline__ int wave_max(int x) {
-#define SOL_STEP(ctrl, rows) x = max(x, __builtin_amdgcn_update_dpp(x, x, ctrl, rows, 0xf, false))
+// Largest value of a wave's lanes, none below 0.
+__device__ __forceinline__ float wave_max(float x) {
+#define SOL_STEP(ctrl, rows)                                                                                              \
+    x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, rows, 0xf, false)))
     SOL_STEP(0x111, 0xf);
     SOL_STEP(0x112, 0xf);
     SOL_STEP(0x114, 0xf);
@@ -112,47 +116,54 @@ __device__ __forceinline__ int wave_max(int x) {
 }
 
 // Pages of a piece, at most, by which `tiles` tiles of `pages` pages in all become no more pieces than fill the slots k times.
-__device__ __forceinline__ int pages_for(float pages, unsigned tiles, int slots, int k) {
-    const float room = (float)slots * (float)k - (float)tiles;   // each tile rounds up by one piece at most
+__device__ __forceinline__ int pages_for(float pages, float tiles, int slots, int k) {
+    const float room = (float)slots * (float)k - tiles;   // each tile rounds up by one piece at most
     return room < 1.f ? 1 << 30 : (int)fmaxf(ceilf(pages / room), (float)kLeastPages);
 }
 
-// Every tile of every request is cut into equal pieces of at most `per` pages.  With few tiles, the pieces fill the slots once; otherwise
-// `per` is chosen among fillings of one to kRounds times by the rounds that the pieces take and the longest piece.  Past 64
-// requests (a second load for each lane) it is two fillings, or no cut at all.
-//
-// Piece `id` (BY_TILE: share 0 of tile `id`); false past the last.  Pieces go by request, head, share, tile.  By the lanes of
-// one wave, on values that all waves of the launch and of the join see alike.
-template <bool BY_TILE>
-__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& part, unsigned id, bool spread, Piece& out) {
+// Pages of a piece, at most: every tile of every request is cut into equal pieces of no more.  With few tiles, the pieces fill the slots
+// once; with many, it is chosen among fillings of one to kRounds times by the time that pieces dealt to free slots take, their
+// mean share and half a piece.  Past 64 requests (more loads for each lane) it is two fillings, or no cut at all.  By the
+// lanes of one wave, on values that all waves of a launch see alike.  `planned`: the choice as another launch made it (not read
+// where it is quicker formed again than fetched from memory that another die wrote).  r: the lane's request, of up to 64.
+__device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& part, const int* planned, Request& r) {
     const int lane = threadIdx.x & 63, G = a.Hq / a.Hk;
-    float sum = 0.f;
-    unsigned tiles = 0;
-    Request r = {};
+    float sum = 0.f, tiles = 0.f;
+    r = Request{};
     for (int s = lane; s < a.S; s += 64) {
-        r = request(a, part, s, G);   // of up to 64 requests, each lane's own
+        r = request(a, part, s, G);
         sum += (float)r.tiles * (float)r.pages;
-        tiles += (unsigned)r.tiles;
+        tiles += (float)r.tiles;
     }
     sum = at_lane(scan_add(sum), 63) * (float)a.Hk;
-    tiles = at_lane(scan_add(tiles), 63) * a.Hk;
+    tiles = at_lane(scan_add(tiles), 63) * (float)a.Hk;
     int per = pages_for(sum, tiles, part.slots, a.S > 64 ? 2 : 1);
-    if (a.S <= 64 && tiles > (unsigned)part.slots / 2) {
+    if (a.S <= 64 && tiles > 0.5f * (float)part.slots) {
+        if (planned) return *planned;
+        const float mine = (float)r.tiles * (float)a.Hk, pages = (float)r.pages;
         float least = INFINITY;
         for (int k = 1; k <= kRounds; ++k) {
-            const int p = pages_for(sum, tiles, part.slots, k), chunks = (r.pages + p - 1) / p;
-            const unsigned pieces = at_lane(scan_add((unsigned)(r.tiles * chunks)), 63) * a.Hk;
-            const int longest = wave_max(r.tiles ? (r.pages + chunks - 1) / chunks : 0);
-            const float cost = (float)((pieces + part.slots - 1) / part.slots) * (float)(longest + part.cost);
+            const int p = pages_for(sum, tiles, part.slots, k);
+            const float chunks = fmaxf(ceilf(pages / (float)p), 1.f);
+            const float pieces = at_lane(scan_add(mine * chunks), 63), longest = wave_max(r.tiles ? pages / chunks : 0.f);
+            const float cost = (sum + pieces * (float)part.cost) / (float)part.slots + 0.5f * (longest + (float)part.cost);
             if (cost < least) least = cost, per = p;
         }
     }
+    return per;
+}
+
+// Piece `id` (BY_TILE: share 0 of tile `id`) of a launch whose pieces have up to `per` pages; false past the last.  Pieces go by
+// request, head, share, tile.  By the lanes of one wave; r as plan_pages() leaves it.
+template <bool BY_TILE>
+__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& part, int per, Request r, unsigned id, bool spread, Piece& out) {
+    const int lane = threadIdx.x & 63, G = a.Hq / a.Hk;
     if (spread) {
         // neighbouring workgroups run on different dies: give each die a run of neighbouring pieces, which share keys
         unsigned total = 0;
         for (int s = lane; s < a.S; s += 64) {
             if (a.S > 64) r = request(a, part, s, G);
-            total += (unsigned)(r.tiles * ((r.pages + per - 1) / per)) * a.Hk;
+            total += (unsigned)(r.tiles * (r.pages / per + (r.pages % per != 0))) * a.Hk;
         }
         total = at_lane(scan_add(total), 63);
         const unsigned run = (total + 7) / 8;
@@ -163,7 +174,7 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& p
     for (int s0 = 0; s0 < a.S; s0 += 64) {
         const int s = s0 + lane;
         if (a.S > 64) r = s < a.S ? request(a, part, s, G) : Request{};
-        const int chunks = (r.pages + per - 1) / per;
+        const int chunks = r.pages / per + (r.pages % per != 0);
         const unsigned pieces = (unsigned)(r.tiles * chunks) * a.Hk;
         const unsigned mine = BY_TILE ? (unsigned)r.tiles * a.Hk : pieces;
         const unsigned slot_upto = scan_add(pieces), upto = BY_TILE ? scan_add(mine) : slot_upto;
@@ -196,13 +207,24 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, const Part& p
     return false;
 }
 
-// find_piece() by the first wave of a workgroup, for all.
-template <bool BY_TILE>
-__device__ __forceinline__ bool find_piece_shared(const CacheAttnArgs& a, const Part& part, unsigned id, bool spread, Piece& out) {
+// A part's workspace: the pages of a piece, then the pieces' results.
+struct PartSpace {
+    int per;
+    int unused[63];
+    float results[1];
+};
+constexpr size_t kPartHeader = offsetof(PartSpace, results);
+
+// The piece of a workgroup, found by its first wave.  The attention kernel plans, and leaves the plan to the join.
+template <bool JOIN>
+__device__ __forceinline__ bool find_piece_shared(const CacheAttnArgs& a, const Part& part, PartSpace* ws, unsigned id, bool spread, Piece& out) {
     __shared__ Piece s_piece;
     __shared__ int s_found;
     if (threadIdx.x < 64) {
-        const bool found = find_piece<BY_TILE>(a, part, id, spread, out);
+        Request r;
+        const int per = plan_pages(a, part, JOIN ? &ws->per : nullptr, r);
+        if (!JOIN && id == 0 && ws && threadIdx.x == 0) ws->per = per;
+        const bool found = find_piece<JOIN>(a, part, per, r, id, spread, out);
         if (threadIdx.x == 0) s_piece = out, s_found = found;
     }
     __syncthreads();
@@ -319,16 +341,16 @@ __device__ __forceinline__ void store_run(void* out, long long at, f32x4 v, int 
     }
 }
 
-// Eight f16 values (keys) of each channel of a lane's bytes: `n` dwords of a key's codes interleaved as in the cache.  BYTES: bytes
-// of a key (two channels each).  scale[k]: exponent of key k, as a float of which the conversion reads the exponent only.
-template <int BYTES>
-__device__ __forceinline__ void values_f16(const u32x4 v, const float (&scale)[8], f16x8 (&out)[2 * BYTES]) {
-#define SOL_CVT(w, s, sel) __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, sel)
+// f16 values of 2 N keys of each channel of a lane's bytes, BYTES bytes (two channels each) a key.  scale[k]: exponent of key k, as a
+// float of which the conversion reads the exponent only.  out[c]: channel c's keys, two a dword.
+template <int BYTES, int N>
+__device__ __forceinline__ void values_f16(const uint32_t* v, const float* scale, uint32_t (&out)[2 * BYTES][N]) {
+#define SOL_CVT(w, s, sel) __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, sel))
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {   // keys 2j, 2j + 1
+    for (int j = 0; j < N; ++j) {   // keys 2j, 2j + 1
 #pragma unroll
         for (int b = 0; b < BYTES; ++b) {
-            f16x2 x, y;
+            uint32_t x, y;
             if constexpr (BYTES == 2) {
                 x = b ? SOL_CVT(v[j], scale[2 * j], 1) : SOL_CVT(v[j], scale[2 * j], 0);
                 y = b ? SOL_CVT(v[j], scale[2 * j + 1], 3) : SOL_CVT(v[j], scale[2 * j + 1], 2);
@@ -336,21 +358,18 @@ __device__ __forceinline__ void values_f16(const u32x4 v, const float (&scale)[8
                 x = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j], 2) : SOL_CVT(v[j >> 1], scale[2 * j], 0);
                 y = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j + 1], 3) : SOL_CVT(v[j >> 1], scale[2 * j + 1], 1);
             }
-            out[2 * b][2 * j] = x[0], out[2 * b][2 * j + 1] = y[0];
-            out[2 * b + 1][2 * j] = x[1], out[2 * b + 1][2 * j + 1] = y[1];
+            out[2 * b][j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            out[2 * b + 1][j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
     }
 #undef SOL_CVT
 }
 
-__device__ __forceinline__ void scales_of(u32x2 b, float (&scale)[8]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        scale[4 * i + 0] = __uint_as_float(b[i] << 23);
-        scale[4 * i + 1] = __uint_as_float(b[i] << 15);
-        scale[4 * i + 2] = __uint_as_float(b[i] << 7);
-        scale[4 * i + 3] = __uint_as_float(b[i] >> 1);
-    }
+__device__ __forceinline__ void scales_of(uint32_t b, float* scale) {
+    scale[0] = __uint_as_float(b << 23);
+    scale[1] = __uint_as_float(b << 15);
+    scale[2] = __uint_as_float(b << 7);
+    scale[3] = __uint_as_float(b >> 1);
 }
 
 // Probabilities as f16 operands, rounded to nearest (F32T: two terms), and their sum, in f32, added to l.  (A sum of the rounded ones by
@@ -528,7 +547,8 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
             for (int e = 0; e < 2; ++e)
                 cut_pair<F32T>(__builtin_amdgcn_exp2f(s[2 * w + b][2 * e]), __builtin_amdgcn_exp2f(s[2 * w + b][2 * e + 1]), ph, pl, 2 * b + e, l);
         float vs[8];
-        scales_of(pg.vs[w], vs);
+        scales_of(pg.vs[w][0], vs);
+        scales_of(pg.vs[w][1], vs + 4);
         if constexpr (EDGE) {   // what lies behind the last token may be anything: a finite scale keeps 0 v = 0
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -537,15 +557,20 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
             // 16 bytes: eight keys of two bytes (d = 128), or two runs of eight bytes (d = 64)
-            f16x8 va[4];
+            uint32_t w16[4][4];
+            const uint32_t bytes[4] = {pg.v[w][c][0], pg.v[w][c][1], pg.v[w][c][2], pg.v[w][c][3]};
             if constexpr (D == 128) {
-                values_f16<2>(pg.v[w][c], vs, va);
+                values_f16<2, 4>(bytes, vs, w16);
             } else {
-                f16x8 x[2], y[2];
-                values_f16<1>(u32x4{pg.v[w][c][0], pg.v[w][c][1], 0, 0}, vs, x);
-                values_f16<1>(u32x4{pg.v[w][c][2], pg.v[w][c][3], 0, 0}, vs, y);
-                va[0] = x[0], va[1] = x[1], va[2] = y[0], va[3] = y[1];
+                uint32_t x[2][4], y[2][4];
+                values_f16<1, 4>(bytes, vs, x);
+                values_f16<1, 4>(bytes + 2, vs, y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w16[0][i] = x[0][i], w16[1][i] = x[1][i], w16[2][i] = y[0][i], w16[3][i] = y[1][i];
             }
+            f16x8 va[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) va[t] = __builtin_bit_cast(f16x8, u32x4{w16[t][0], w16[t][1], w16[t][2], w16[t][3]});
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 o[4 * c + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[t], ph, o[4 * c + t], 0, 0, 0);
@@ -556,13 +581,17 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2) {
+__global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
+                                                                                        PartSpace* ws) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, CT = D / 16;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece<false>(a, part, blockIdx.x, false, pc)) return;
+    Request request_of_lane;
+    const int per = plan_pages(a, part, nullptr, request_of_lane);
+    if (blockIdx.x == 0 && ws && lane == 0) ws->per = per;
+    if (!find_piece<false>(a, part, per, request_of_lane, blockIdx.x, false, pc)) return;
 
     const int r = pc.tile * kFewTile + j;
     const bool valid = r < pc.rows;
@@ -630,7 +659,7 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
                 store_run<F32T, VEC>(a.out, oi + CT * (4 * g + e) + t, f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]} * inv, 4);
         return;
     }
-    float* to = static_cast<float*>(a.ws) + (long long)blockIdx.x * (kFewTile * (D + 2));
+    float* to = ws->results + (long long)blockIdx.x * (kFewTile * (D + 2));
     if (g == 0) to[2 * j] = most < 0.f ? kLowest : m, to[2 * j + 1] = l;
     float* po = to + 2 * kFewTile + j * D;
 #pragma unroll
@@ -656,54 +685,61 @@ struct Stage {
     uint32_t ks[64];                // scale bytes [chunk][window] of a lane
 };
 
-template <int D>
-struct ManyPage {                   // a thread's part of a page
-    u32x4 k, v;
-    u32x2 vs;
-    uint32_t ks;
+// A thread's part of a page: the first 256 threads (d = 64: 128) 16 bytes of keys, and thread t of 256 N the values of 8 / N keys of
+// the channel run i.
+template <int D, int N>
+struct ManyPage {
+    u32x4 k;
+    uint32_t v[4 / N], vs[2 / N], ks;
 };
 
-template <int D>
-__device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D>& r) {
+template <int D, int N>
+__device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D, N>& r) {
     using L = PageLayout<D>;
-    const int t = threadIdx.x, lane = t & 63, i = lane & 31, h = lane >> 5;
-    if (D == 128 || t < 128) {
-        const int w = D == 128 ? t >> 7 : t >> 6, c = D == 128 ? (t >> 6) & 1 : 0;
-        r.k = *reinterpret_cast<const u32x4*>(page + L::k + (32 * w + swap23(i)) * (D / 2) + (2 * c + h) * 16);
+    const unsigned t = threadIdx.x, lane = t & 63, i = lane & 31, h = lane >> 5;
+    if (t < 2 * D) {
+        const unsigned w = D == 128 ? t >> 7 : t >> 6, c = D == 128 ? (t >> 6) & 1 : 0;
+        r.k = *reinterpret_cast<const u32x4*>(page + (L::k + (32 * w + swap23(i)) * (D / 2) + (2 * c + h) * 16));
     }
-    // thread t: keys 8 (t >> 5) ..., channel run t & 31
-    if constexpr (D == 128) {
-        r.v = *reinterpret_cast<const u32x4*>(page + L::v + t * 16);
-    } else {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(page + L::v + t * 8);
-        r.v = u32x4{x[0], x[1], 0, 0};
-    }
-    r.vs = *reinterpret_cast<const u32x2*>(page + L::vs + ((t >> 5) * (D / 32) + (t & 31) / (1024 / D)) * 8);
+    // d = 128: 16 / N bytes, d = 64: 8 / N
+    const uint32_t* v = reinterpret_cast<const uint32_t*>(page + (L::v + t * (D / (8 * N))));
+#pragma unroll
+    for (int x = 0; x < D / (32 * N); ++x) r.v[x] = v[x];
+    const unsigned oct = t / (32 * N), run = t / N % 32, part = t % N;
+    const uint32_t* vs = reinterpret_cast<const uint32_t*>(page + (L::vs + (oct * (D / 32) + run / (1024 / D)) * 8 + part * 4));
+#pragma unroll
+    for (int x = 0; x < 2 / N; ++x) r.vs[x] = vs[x];
     if (t < 64) {
-        if constexpr (D == 128) r.ks = *reinterpret_cast<const uint32_t*>(page + L::ks + t * 4);
-        else r.ks = *reinterpret_cast<const uint16_t*>(page + L::ks + t * 2);
+        if constexpr (D == 128) r.ks = *reinterpret_cast<const uint32_t*>(page + (L::ks + t * 4));
+        else r.ks = *reinterpret_cast<const uint16_t*>(page + (L::ks + t * 2));
     }
 }
 
 // left: tokens of the page that there are; what lies behind them may be anything, and a finite scale keeps 0 v = 0.
-template <int D>
-__device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, int left) {
+template <int D, int N>
+__device__ __forceinline__ void many_store(const ManyPage<D, N>& r, Stage<D>& st, int left) {
     constexpr int CT = D / 32;
-    const int t = threadIdx.x;
-    if (D == 128 || t < 128) st.k[t] = r.k;
+    const unsigned t = threadIdx.x;
+    if (t < 2 * D) st.k[t] = r.k;
     if (t < 64) st.ks[t] = r.ks;
-    float vs[8];
-    scales_of(r.vs, vs);
+    const unsigned oct = t / (32 * N), run = t / N % 32, part = t % N;
+    float vs[8 / N];
+#pragma unroll
+    for (int x = 0; x < 2 / N; ++x) scales_of(r.vs[x], vs + 4 * x);
     if (left < kPage) {
+        asm volatile("" : "+s"(left));
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (8 * (t >> 5) + i >= left) vs[i] = 1.0f;
+        for (int i = 0; i < 8 / N; ++i)
+            if ((int)(8 * oct + 8 / N * part) + i >= left) vs[i] = 1.0f;
     }
-    f16x8 va[CT];
-    values_f16<D / 64>(r.v, vs, va);
-    const int u = t >> 6, lane = t & 63;   // keys 16u + 8h ...
+    uint32_t va[CT][4 / N];
+    values_f16<D / 64, 4 / N>(r.v, vs, va);
 #pragma unroll
-    for (int c = 0; c < CT; ++c) st.v[(u * CT + c) * 64 + lane] = va[c];
+    for (int c = 0; c < CT; ++c) {   // keys 16 (oct / 2) + 8 (oct % 2) ...
+        uint32_t* to = reinterpret_cast<uint32_t*>(&st.v[((oct >> 1) * CT + c) * 64 + (oct & 1) * 32 + run]) + part * (4 / N);
+        if constexpr (N == 1) *reinterpret_cast<u32x4*>(to) = u32x4{va[c][0], va[c][1], va[c][2], va[c][3]};
+        else *reinterpret_cast<u32x2*>(to) = u32x2{va[c][0], va[c][1]};
+    }
 }
 
 template <int D, bool F32T>
@@ -783,15 +819,16 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2, float* ws) {
+__global__ __launch_bounds__(64 * kManyWaves, 8 / kManyWaves * (kManyWaves / 4)) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
+                                                                                                       PartSpace* ws) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
     __shared__ Stage<D> stage[2];
-    __shared__ int s_last[4];
+    __shared__ int s_last[kManyWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece_shared<false>(a, part, blockIdx.x, true, pc)) return;
+    if (!find_piece_shared<false>(a, part, ws, blockIdx.x, true, pc)) return;
     const unsigned slot = pc.slot0 + (unsigned)pc.chunk * pc.tiles;
 
     const int r = pc.tile * kManyTile + 32 * wave + j;
@@ -818,7 +855,9 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     least = __builtin_amdgcn_readfirstlane(least);
     if (lane == 0) s_last[wave] = last;
     __syncthreads();
-    const int all = max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3]));
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kManyWaves; ++w) all = max(all, s_last[w]);
     Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, __builtin_amdgcn_readfirstlane(min(pc.p1, (all + kPage - 1) / kPage)));
     const long long page_stride = (long long)a.Hk * L::bytes;
     const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
@@ -833,14 +872,15 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     for (int i = 0; i < 16; ++i) off[i] = kShift;
 
     // the page of tokens key0 ... is in stage[turn], the one after it in registers
-    ManyPage<D> pg;
+    constexpr int N = kManyWaves / 4;
+    ManyPage<D, N> pg;
     int id = pages.next(), turn = 0, key0 = pages.p * kPage;
     bool more = id >= 0;
     if (more) {
-        many_load<D>(store + id * page_stride, pg);
-        many_store<D>(pg, stage[0], pc.len - key0);
+        many_load<D, N>(store + id * page_stride, pg);
+        many_store<D, N>(pg, stage[0], pc.len - key0);
         id = pages.next();
-        if (id >= 0) many_load<D>(store + id * page_stride, pg);
+        if (id >= 0) many_load<D, N>(store + id * page_stride, pg);
     }
     __syncthreads();
     while (more) {
@@ -848,9 +888,9 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
         more = id >= 0;
         if (more) {
             key0 = pages.p * kPage;
-            many_store<D>(pg, stage[turn ^ 1], pc.len - key0);
+            many_store<D, N>(pg, stage[turn ^ 1], pc.len - key0);
             id = pages.next();
-            if (id >= 0) many_load<D>(store + id * page_stride, pg);
+            if (id >= 0) many_load<D, N>(store + id * page_stride, pg);
         }
         if (now < last) many_page<D, F32T>(stage[turn], q, now, now + kPage > least, sees, m, most, off, l, o);
         turn ^= 1;
@@ -872,7 +912,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
         return;
     }
     if (slot >= gridDim.x) return;   // rows that overlap: no room was asked for
-    float* to = ws + (long long)slot * (kManyTile * (D + 2));
+    float* to = ws->results + (long long)slot * (kManyTile * (D + 2));
     const int row = 32 * wave + j;
     if (h == 0) to[2 * row] = most < 0.f ? kLowest : m, to[2 * row + 1] = l;
     float* po = to + 2 * kManyTile + row * D;
@@ -883,54 +923,70 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
 }
 
 // ---------------------------------------------------------------------------
-// Joins the shares of a tile's rows, four rows at a time, in an order that the plan fixes.  D / 4 threads hold a row, four channels
-// each; the shares are dealt to several such groups, whose sums are added in LDS.
+// Joins the shares of a tile's rows (gridDim.y workgroups a tile, of the few for four rows each), in an order that the plan fixes.  D / 4 threads hold a row, four
+// channels each; where there are fewer rows than groups, the shares are dealt to several groups, whose sums are added in LDS.  Bound
+// by latency: the plan, the maxima, the sums.
 // ---------------------------------------------------------------------------
-constexpr int kJoinRows = 4, kJoinThreads = 512;
+constexpr int kJoinThreads = 512;
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttnArgs a, const Part part, const unsigned pieces, const float* ws) {
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttnArgs a, const Part part, const unsigned pieces, PartSpace* ws) {
     constexpr int LANES = D / 4, GROUPS = kJoinThreads / LANES;
     __shared__ f32x4 s_o[GROUPS][LANES];
     __shared__ float s_l[GROUPS];
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece_shared<true>(a, part, blockIdx.x, false, pc) || pc.chunks == 1) return;
+    if (!find_piece_shared<true>(a, part, ws, blockIdx.x, false, pc) || pc.chunks == 1) return;
     if (pc.slot0 + (uint64_t)(pc.chunks - 1) * pc.tiles >= pieces) return;   // rows that overlap: no room was asked for
     const long long stride = (long long)pc.tiles * (part.tile * (D + 2));
-    const float* const tile = ws + (long long)pc.slot0 * (part.tile * (D + 2));
+    const float* const tile = ws->results + (long long)pc.slot0 * (part.tile * (D + 2));
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    for (int row0 = kJoinRows * blockIdx.y; row0 < part.tile; row0 += kJoinRows * gridDim.y) {
-        const int first = pc.tile * part.tile + row0, rows = min(pc.rows - first, kJoinRows);
-        if (rows <= 0) return;
-        const float* at = tile + 2 * row0;   // (max, sum) pairs of the rows
-        const float* ot = tile + 2 * part.tile + row0 * D;
-        const int width = rows <= 2 ? rows : kJoinRows, shares = GROUPS / width;
-        const int j = group % width, share = group / width;
+    const int each = part.tile == kFewTile ? 4 : part.tile / gridDim.y, row0 = each * blockIdx.y, first = pc.tile * part.tile + row0;
+    const int rows = min(pc.rows - first, each);   // of this workgroup
+    int width = 1;   // rows at a time, a power of two
+    while (width < GROUPS && width < rows) width *= 2;
+    const int shares = GROUPS / width, share = group / width;
+    for (int j0 = 0; j0 < rows; j0 += width) {
+        const int j = j0 + group % width;
+        const float* at = tile + 2 * (row0 + j);   // (max, sum) pairs of the rows
+        const float* ot = tile + 2 * part.tile + (row0 + j) * D + 4 * lane;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
         float l = 0.f;
         if (j < rows) {
             float top = kLowest;
-            for (int c = lane; c < pc.chunks; c += LANES) top = fmaxf(top, at[c * stride + 2 * j]);
+            for (int c = lane; c < pc.chunks; c += LANES) top = fmaxf(top, at[c * stride]);
 #pragma unroll
             for (int x = 1; x < LANES; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-#pragma unroll 4
-            for (int c = share; c < pc.chunks; c += shares) {
-                const float w = __builtin_amdgcn_exp2f(at[c * stride + 2 * j] - top);
-                l += w * at[c * stride + 2 * j + 1];
-                o += w * *reinterpret_cast<const f32x4*>(ot + c * stride + j * D + 4 * lane);
+            for (int c0 = share; c0 < pc.chunks; c0 += 4 * shares) {   // the loads of four shares at a time
+                f32x2 ml[4];
+                f32x4 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const long long c = min(c0 + i * shares, pc.chunks - 1) * stride;
+                    ml[i] = *reinterpret_cast<const f32x2*>(at + c);
+                    v[i] = *reinterpret_cast<const f32x4*>(ot + c);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = c0 + i * shares < pc.chunks ? __builtin_amdgcn_exp2f(ml[i][0] - top) : 0.f;
+                    l += c0 + i * shares < pc.chunks ? w * ml[i][1] : 0.f;   // what is read twice may be infinite
+                    o += c0 + i * shares < pc.chunks ? w * v[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+                }
             }
         }
-        s_o[group][lane] = o;
-        if (lane == 0) s_l[group] = l;
-        __syncthreads();
+        if (shares > 1) {
+            __syncthreads();   // the sums of the rows before have been read
+            s_o[group][lane] = o;
+            if (lane == 0) s_l[group] = l;
+            __syncthreads();
+            if (share == 0)
+                for (int x = 1; x < min(shares, pc.chunks); ++x) o += s_o[group + x * width][lane], l += s_l[group + x * width];
+        }
         if (share == 0 && j < rows) {
-            for (int x = 1; x < min(shares, pc.chunks); ++x) o += s_o[j + x * width][lane], l += s_l[j + x * width];
             const float inv = l == 0.f ? 0.f : 1.0f / l;
             const int r = first + j;
             store_run<F32T, VEC>(a.out, (pc.hk * G + r % G) * a.so.h + (pc.row0 + r / G) * a.so.n + 4 * lane, o * inv, 4);
         }
-        __syncthreads();
     }
 }
 
@@ -956,6 +1012,7 @@ struct Plan {
     bool use_few, use_many;
     long long few_pieces, many_pieces, few_tiles, many_tiles;
     size_t few_bytes, many_bytes;
+    int few_quads;   // fours of rows of a tile of the few, at most
 };
 
 // Which kernels a call needs: requests of up to kFewRows rows go to the one for few rows, unless there is one request only, whose
@@ -970,14 +1027,15 @@ Plan make_plan(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages)
     const bool join = max_pages > kLeastPages;   // otherwise a tile is one piece
     if (p.use_few) {
         const int rows = p.use_many ? std::min(max_rows, std::max(1, kFewRows / (Hq / Hk))) : max_rows;
+        p.few_quads = (int)(std::min<long long>((long long)rows * (Hq / Hk), kFewTile) + 3) / 4;
         p.few_pieces = most_pieces(p.few, S, T, rows, Hq, Hk, max_pages);
         p.few_tiles = most_tiles(p.few, S, T, rows, Hq, Hk);
-        p.few_bytes = join ? (size_t)p.few_pieces * kFewTile * (d + 2) * sizeof(float) : 0;
+        p.few_bytes = join ? kPartHeader + (size_t)p.few_pieces * kFewTile * (d + 2) * sizeof(float) : 0;
     }
     if (p.use_many) {
         p.many_pieces = (most_pieces(p.many, S, T, max_rows, Hq, Hk, max_pages) + 7) / 8 * 8;
         p.many_tiles = most_tiles(p.many, S, T, max_rows, Hq, Hk);
-        p.many_bytes = join ? (size_t)p.many_pieces * kManyTile * (d + 2) * sizeof(float) : 0;
+        p.many_bytes = join ? kPartHeader + (size_t)p.many_pieces * kManyTile * (d + 2) * sizeof(float) : 0;
     }
     return p;
 }
@@ -992,14 +1050,15 @@ size_t cache_attn_workspace_bytes(int S, int T, int max_rows, int Hq, int Hk, in
 template <int D, bool F32T, bool VEC>
 static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) {
     const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)a.d));
-    float* many_ws = a.ws ? reinterpret_cast<float*>(static_cast<char*>(a.ws) + p.few_bytes) : nullptr;
+    PartSpace* few_ws = p.few_bytes ? static_cast<PartSpace*>(a.ws) : nullptr;
+    PartSpace* many_ws = p.many_bytes ? reinterpret_cast<PartSpace*>(static_cast<char*>(a.ws) + p.few_bytes) : nullptr;
     hipError_t e = hipSuccess;
     if (p.use_many) {
-        cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 256, 0, st>>>(a, p.many, scale_log2, many_ws);
+        cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 64 * kManyWaves, 0, st>>>(a, p.many, scale_log2, many_ws);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.use_few) {
-        cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_pieces, 64, 0, st>>>(a, p.few, scale_log2);
+        cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_pieces, 64, 0, st>>>(a, p.few, scale_log2, few_ws);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.many_bytes) {
@@ -1007,7 +1066,7 @@ static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) 
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.few_bytes) {
-        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.few_tiles, kFewTile / kJoinRows), kJoinThreads, 0, st>>>(a, p.few, (unsigned)p.few_pieces, static_cast<const float*>(a.ws));
+        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.few_tiles, (unsigned)p.few_quads), kJoinThreads, 0, st>>>(a, p.few, (unsigned)p.few_pieces, few_ws);
         e = hipGetLastError();
     }
     return e;
