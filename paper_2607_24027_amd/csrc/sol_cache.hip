@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const RopeArgs a, con
 // New entries lie behind the used part of a table row and in front of the ring, pages that come back behind the ring's
 // last: no workgroup reads what another writes.
 // ---------------------------------------------------------------------------
-constexpr int kTablesThreads = 1024, kTablesRows = 4096;
+constexpr int kTablesThreads = 1024, kTablesRows = 2048;
 
 // First index with sum[i] > x, of n ascending sums.
 __device__ __forceinline__ int upper_bound(const int* sum, int n, int x) {
@@ -247,7 +247,9 @@ __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const Tabl
         a.table[(long long)s * MP + page] = fresh(r);
     }
     const int total_rows = s_rows[S - 1];
-    for (int t = blockIdx.x * kTablesRows + tid; t < min(a.rows, (int)(blockIdx.x + 1) * kTablesRows); t += kTablesThreads) {
+    // the first of several workgroups has no rows: it has the pages that come back
+    const int part = gridDim.x > 1 ? (int)blockIdx.x - 1 : 0;
+    for (int t = part * kTablesRows + tid; part >= 0 && t < min(a.rows, (part + 1) * kTablesRows); t += kTablesThreads) {
         int slot = -1, pos = -1;
         if (t < total_rows) {
             const int s = upper_bound(s_rows, S, t);
@@ -263,28 +265,43 @@ __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const Tabl
         a.positions[t] = pos;
     }
     if (blockIdx.x) return;
-    // Pages that come back, in order: the valid ones of 1,024 entries at a time.
+    // Pages that come back, in order: the valid ones of 8,192 entries at a time, eight to a thread.
     const int total_gone = s_gone[S - 1];
     int base = 0;
-    for (int r0 = 0; r0 < total_gone; r0 += kTablesThreads) {
-        const int r = r0 + tid;
-        int page = -1;
-        if (r < total_gone) {
-            const int s = upper_bound(s_gone, S, r);
-            const int before = (held(s) + kPage - 1) / kPage;
-            page = a.table[(long long)s * MP + before - (s_gone[s] - r)];
+    for (int r0 = 0; r0 < total_gone; r0 += 8 * kTablesThreads) {
+        const int first = r0 + 8 * tid;
+        int page[8], valid = 0;
+        int s = first < total_gone ? upper_bound(s_gone, S, first) : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            page[i] = -1;
+            if (first + i < total_gone) {
+                while (s_gone[s] <= first + i) ++s;
+                page[i] = a.table[(long long)s * MP + (held(s) + kPage - 1) / kPage - (s_gone[s] - first - i)];
+            }
         }
-        const bool valid = page >= 0 && page < P;
-        const uint64_t m = __ballot(valid);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) valid += page[i] >= 0 && page[i] < P;
+        int upto = valid;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const int x = __shfl_up(upto, m);
+            if (lane >= m) upto += x;
+        }
         __syncthreads();
-        if (lane == 0) w_need[wave] = __popcll(m);
+        if (lane == 63) w_need[wave] = upto;
         __syncthreads();
-        int rank = base + __popcll(m & ((1ull << lane) - 1));
+        int rank = base + upto - valid;
         for (int w = 0; w < 16; ++w) {
             if (w < wave) rank += w_need[w];
             base += w_need[w];
         }
-        if (valid && rank < P - count) a.ring[(int)(((long long)head + count + rank) % P)] = page;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (page[i] < 0 || page[i] >= P) continue;
+            if (rank < P - count) a.ring[(int)(((long long)head + count + rank) % P)] = page[i];
+            ++rank;
+        }
     }
     if (tid == 0) {
         a.state_out[0] = (int)(((long long)head + taken) % P);
@@ -293,8 +310,10 @@ __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const Tabl
 }
 
 // ---------------------------------------------------------------------------
-// Append.  D / 4 lanes hold a token of a head, half of them its key and half its value, eight channels each; four
-// lanes share a scale.
+// Append and read-back: a wave takes eight tokens of a head.  Keys: lane 8j + p holds channels D/8 p ... of token j, whose codes
+// lie side by side in the page.  Values: lane 8r + j holds the channel runs r, r + 8, r + 16, r + 24 of token j, so that tokens
+// in a row, whose codes of a run are neighbouring bytes in the page, leave in one piece (3,600 tokens of 40 heads:
+// 31 us with a token's values on neighbouring lanes).
 // ---------------------------------------------------------------------------
 template <int D>
 __device__ __forceinline__ int k_scale_at(int tok, int group) {   // byte of a group's scale inside the key scales
@@ -302,107 +321,226 @@ __device__ __forceinline__ int k_scale_at(int tok, int group) {   // byte of a g
     return (((group & 1) * 32 + swapped) * (D / 64) + (group >> 1)) * 2 + (tok >> 5);
 }
 
+// N consecutive elements, N = 2 or a multiple of 4.
+template <class E, bool VEC, int N>
+__device__ __forceinline__ void load_run(const void* p, long long at, float (&x)[N]) {
+    if constexpr (N == 2) {
+        if constexpr (E::size == 2) {
+            const uint16_t* q = static_cast<const uint16_t*>(p) + at;
+            if constexpr (VEC) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(q);
+                x[0] = __uint_as_float(w << 16), x[1] = __uint_as_float(w & 0xffff0000u);
+            } else {
+                x[0] = bf16_to_f32(q[0]), x[1] = bf16_to_f32(q[1]);
+            }
+        } else {
+            const float* q = static_cast<const float*>(p) + at;
+            if constexpr (VEC) {
+                const f32x2 w = *reinterpret_cast<const f32x2*>(q);
+                x[0] = w[0], x[1] = w[1];
+            } else {
+                x[0] = q[0], x[1] = q[1];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const f32x4 v = load4<E, VEC>(p, at + i);
+            x[i] = v[0], x[i + 1] = v[1], x[i + 2] = v[2], x[i + 3] = v[3];
+        }
+    }
+}
+
+template <class E, bool VEC, int N>
+__device__ __forceinline__ void store_run(void* p, long long at, const float (&x)[N]) {
+    if constexpr (N == 2) {
+        if constexpr (E::size == 2) {
+            uint16_t* q = static_cast<uint16_t*>(p) + at;
+            const uint32_t a = f32_to_bf16(x[0]), b = f32_to_bf16(x[1]);
+            if constexpr (VEC) *reinterpret_cast<uint32_t*>(q) = a | (b << 16);
+            else q[0] = (uint16_t)a, q[1] = (uint16_t)b;
+        } else {
+            float* q = static_cast<float*>(p) + at;
+            if constexpr (VEC) *reinterpret_cast<f32x2*>(q) = f32x2{x[0], x[1]};
+            else q[0] = x[0], q[1] = x[1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) store4<E, VEC>(p, at + i, f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]});
+    }
+}
+
+// Magnitudes order as integers, NaN above infinity.
+template <int N>
+__device__ __forceinline__ uint32_t magnitude(const float (&x)[N]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    return top;
+}
+
+// floor(log2 m) - 2, one more past 7/4 of the power of two: adding 2^21 - 1 to the bits carries from 1.75 + 1 ulp on.
+__device__ __forceinline__ int exponent_of(uint32_t top, int lo, int hi) {
+    return min(max((int)((top + 0x1fffffu) >> 23) - 127 - 2, lo), hi);
+}
+
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Eight channels' codes in a dword (fewer: in its low bytes).
+template <int N>
+__device__ __forceinline__ uint32_t encode(const float* x, float scale) {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
+    if constexpr (N >= 4) c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
+    if constexpr (N >= 8) {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
+    }
+    return c;
+}
+
+template <int N>
+__device__ __forceinline__ void decode(uint32_t c, float scale, float* x) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0);
+    x[0] = a[0], x[1] = a[1];
+    if constexpr (N >= 4) {
+        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+        x[2] = b[0], x[3] = b[1];
+    }
+    if constexpr (N >= 8) {
+        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
+        x[4] = b[0], x[5] = b[1], x[6] = d[0], x[7] = d[1];
+    }
+}
+
+// A lane's place in the tokens and in the pages: of its key part (k) and of its value part (v).
+struct Places {
+    int t0, h, jk, p, jv, r, slot_k, slot_v;
+    bool there_k, there_v;   // the token is one of the call, and its slot one of the store
+};
+
+__device__ __forceinline__ bool places(int T, int H, int P, const int32_t* slots, Places& x) {
+    const int lane = threadIdx.x & 63;
+    const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    x.t0 = (int)(item / H) * 8;
+    if (x.t0 >= T) return false;
+    x.h = (int)(item % H);
+    x.jk = lane >> 3, x.p = lane & 7, x.jv = lane & 7, x.r = lane >> 3;
+    x.slot_k = x.t0 + x.jk < T ? slots[x.t0 + x.jk] : -1;
+    x.slot_v = x.t0 + x.jv < T ? slots[x.t0 + x.jv] : -1;
+    x.there_k = x.slot_k >= 0 && x.slot_k / kPage < P;
+    x.there_v = x.slot_v >= 0 && x.slot_v / kPage < P;
+    return true;
+}
+
 template <class E, int D, bool VEC>
 __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
     using L = PageLayout<D>;
-    constexpr int LPT = D / 4, HALF = LPT / 2;
-    const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LPT;
-    const int sub = threadIdx.x % LPT, piece = sub % HALF;
-    const bool is_v = sub >= HALF;
-    if (item >= (long long)a.T * a.H) return;   // whole groups of LPT lanes
-    const int t = (int)(item / a.H), h = (int)(item % a.H);
-    const int slot = a.slots[t];
-    if (slot < 0 || slot / kPage >= a.P) return;
-    const Strides& st = is_v ? a.sv : a.sk;
-    const void* src = is_v ? a.v : a.k;
-    const long long at = h * st.h + t * st.n + 8 * piece;
-    const f32x4 x0 = load4<E, VEC>(src, at), x1 = load4<E, VEC>(src, at + 4);
-    uint32_t top = 0;   // magnitudes order as integers, NaN above infinity
+    constexpr int CK = D / 8, CV = D / 32, GROUPS = D / 32;
+    Places x;
+    if (!places(a.T, a.H, a.P, a.slots, x)) return;   // whole waves
+    float k[CK] = {}, v[4][CV] = {};
+    if (x.there_k) load_run<E, VEC>(a.k, x.h * a.sk.h + (x.t0 + x.jk) * a.sk.n + CK * x.p, k);
+    if (x.there_v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        top = max(top, __float_as_uint(x0[i]) & 0x7fffffffu);
-        top = max(top, __float_as_uint(x1[i]) & 0x7fffffffu);
+        for (int i = 0; i < 4; ++i) load_run<E, VEC>(a.v, x.h * a.sv.h + (x.t0 + x.jv) * a.sv.n + CV * (x.r + 8 * i), v[i]);
     }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    int bad = top >= 0x7f800000u;
+    uint32_t top_k = magnitude(k), top_v[GROUPS];
+    top_k = max(top_k, (uint32_t)__shfl_xor((int)top_k, 1));
+    if constexpr (D == 64) top_k = max(top_k, (uint32_t)__shfl_xor((int)top_k, 2));
 #pragma unroll
-    for (int m = 4; m < LPT; m *= 2) bad |= __shfl_xor(bad, m);
-    // floor(log2 m) - 2, one more past 7/4 of the power of two: adding 2^21 - 1 to the bits carries from 1.75 + 1 ulp on
-    int e = (int)((top + 0x1fffffu) >> 23) - 127 - 2;
-    e = is_v ? min(max(e, -23), 13) : min(max(e, -100), 125);
-    const float scale = __uint_as_float((uint32_t)(e + 127) << 23);
-    uint32_t code = 0;
-    if (!bad) {
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x0[0], x0[1], scale, 0);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x0[2], x0[3], scale, 1);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x1[0], x1[1], scale, 2);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x1[2], x1[3], scale, 3);
+    for (int g = 0; g < GROUPS; ++g) {
+        top_v[g] = D == 128 ? magnitude(v[g]) : max(magnitude(v[2 * g]), magnitude(v[2 * g + 1]));
+#pragma unroll
+        for (int m = 8; m < 64; m *= 2) top_v[g] = max(top_v[g], (uint32_t)__shfl_xor((int)top_v[g], m));
     }
-    uint8_t* page = a.store + ((long long)(slot / kPage) * a.H + h) * L::bytes;
-    const int tok = slot % kPage, group = piece >> 2;
-    const uint8_t byte = bad && !is_v ? 255 : (uint8_t)(e + 127);
-    if (!is_v) {
-        *reinterpret_cast<uint32_t*>(page + L::k + tok * (D / 2) + 4 * piece) = code;
-        if ((piece & 3) == 0) page[L::ks + k_scale_at<D>(tok, group)] = byte;
-    } else {
-        uint8_t* to = page + L::v + ((tok >> 3) * 32 * 8 + (tok & 7)) * (D / 64);
-        if constexpr (D == 128) {
-            *reinterpret_cast<uint16_t*>(to + (2 * piece) * 16) = (uint16_t)code;
-            *reinterpret_cast<uint16_t*>(to + (2 * piece + 1) * 16) = (uint16_t)(code >> 16);
-        } else {
+    // tokens with an infinity or NaN in either part: bit j
+    uint32_t all_v = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) to[(4 * piece + i) * 8] = (uint8_t)(code >> (8 * i));
+    for (int g = 0; g < GROUPS; ++g) all_v = max(all_v, top_v[g]);
+    uint64_t mk = __ballot(top_k >= 0x7f800000u), bad = __ballot(all_v >= 0x7f800000u) & 0xff;
+    if (mk) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bad |= (mk >> (8 * j) & 0xff) ? 1u << j : 0;
+    }
+    if (x.there_k) {
+        uint8_t* page = a.store + ((long long)(x.slot_k / kPage) * a.H + x.h) * L::bytes;
+        const int tok = x.slot_k % kPage, e = exponent_of(top_k, -100, 125);
+        const bool nan = bad >> x.jk & 1;
+        const float scale = power(e);
+        if constexpr (D == 128) *reinterpret_cast<u32x2*>(page + L::k + tok * (D / 2) + 8 * x.p) = u32x2{encode<8>(k, scale), encode<8>(k + 8, scale)};
+        else *reinterpret_cast<uint32_t*>(page + L::k + tok * (D / 2) + 4 * x.p) = encode<8>(k, scale);
+        if (x.p % (32 / CK) == 0) page[L::ks + k_scale_at<D>(tok, x.p / (32 / CK))] = nan ? 255 : (uint8_t)(e + 127);
+    }
+    if (x.there_v) {
+        uint8_t* page = a.store + ((long long)(x.slot_v / kPage) * a.H + x.h) * L::bytes;
+        const int tok = x.slot_v % kPage;
+        const bool nan = bad >> x.jv & 1;
+        uint8_t* to = page + L::v + ((tok >> 3) * 32 * 8 + (tok & 7)) * (D / 64) + x.r * (D / 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t code = nan ? 0 : encode<CV>(v[i], power(exponent_of(top_v[D == 128 ? i : i >> 1], -23, 13)));
+            if constexpr (D == 128) *reinterpret_cast<uint16_t*>(to + 8 * i * (D / 8)) = (uint16_t)code;
+            else to[8 * i * (D / 8)] = (uint8_t)code;
         }
-        if ((piece & 3) == 0) page[L::vs + ((tok >> 3) * (D / 32) + group) * 8 + (tok & 7)] = byte;
+        // lane (r, j) writes the scale of group r
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g)
+            if (x.r == g) page[L::vs + ((tok >> 3) * GROUPS + g) * 8 + (tok & 7)] = nan ? (uint8_t)(127 - 23) : (uint8_t)(exponent_of(top_v[g], -23, 13) + 127);
     }
 }
 
 template <class E, int D, bool VEC>
 __global__ __launch_bounds__(256) void cache_read_kernel(const ReadArgs a) {
     using L = PageLayout<D>;
-    constexpr int LPT = D / 4, HALF = LPT / 2;
-    const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LPT;
-    const int sub = threadIdx.x % LPT, piece = sub % HALF;
-    const bool is_v = sub >= HALF;
-    if (item >= (long long)a.T * a.H || (is_v ? !a.v : !a.k)) return;
-    const int t = (int)(item / a.H), h = (int)(item % a.H);
-    const int slot = a.slots[t];
-    f32x4 x0 = {0.f, 0.f, 0.f, 0.f}, x1 = x0;
-    if (slot >= 0 && slot / kPage < a.P) {
-        const uint8_t* page = a.store + ((long long)(slot / kPage) * a.H + h) * L::bytes;
-        const int tok = slot % kPage, group = piece >> 2;
-        const uint32_t kb = page[L::ks + k_scale_at<D>(tok, group)];
-        uint32_t code, byte = kb;
-        if (!is_v) {
-            code = *reinterpret_cast<const uint32_t*>(page + L::k + tok * (D / 2) + 4 * piece);
-        } else {
-            const uint8_t* from = page + L::v + ((tok >> 3) * 32 * 8 + (tok & 7)) * (D / 64);
+    constexpr int CK = D / 8, CV = D / 32, GROUPS = D / 32;
+    const float not_a_number = __uint_as_float(0x7fc00000u);
+    Places x;
+    if (!places(a.T, a.H, a.P, a.slots, x)) return;
+    if (a.k && x.t0 + x.jk < a.T) {
+        float k[CK] = {};
+        if (x.there_k) {
+            const uint8_t* page = a.store + ((long long)(x.slot_k / kPage) * a.H + x.h) * L::bytes;
+            const int tok = x.slot_k % kPage;
+            const uint32_t byte = page[L::ks + k_scale_at<D>(tok, x.p / (32 / CK))];
+            const float scale = __uint_as_float(byte << 23);
             if constexpr (D == 128) {
-                code = *reinterpret_cast<const uint16_t*>(from + (2 * piece) * 16) |
-                       ((uint32_t)*reinterpret_cast<const uint16_t*>(from + (2 * piece + 1) * 16) << 16);
+                const u32x2 c = *reinterpret_cast<const u32x2*>(page + L::k + tok * (D / 2) + 8 * x.p);
+                decode<8>(c[0], scale, k);
+                decode<8>(c[1], scale, k + 8);
             } else {
-                code = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) code |= (uint32_t)from[(4 * piece + i) * 8] << (8 * i);
+                decode<8>(*reinterpret_cast<const uint32_t*>(page + L::k + tok * (D / 2) + 4 * x.p), scale, k);
             }
-            byte = page[L::vs + ((tok >> 3) * (D / 32) + group) * 8 + (tok & 7)];
+            if (byte == 255) {
+#pragma unroll
+                for (int i = 0; i < CK; ++i) k[i] = not_a_number;
+            }
         }
-        const float scale = __uint_as_float(byte << 23);
-        const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 0), a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 1);
-        const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 2), a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 3);
-        x0 = f32x4{a0[0], a0[1], a1[0], a1[1]};
-        x1 = f32x4{a2[0], a2[1], a3[0], a3[1]};
-        if (kb == 255) {
-            const float nan = __uint_as_float(0x7fc00000u);
-            x0 = x1 = f32x4{nan, nan, nan, nan};
-        }
+        store_run<E, VEC>(a.k, x.h * a.sk.h + (x.t0 + x.jk) * a.sk.n + CK * x.p, k);
     }
-    const Strides& st = is_v ? a.sv : a.sk;
-    void* dst = is_v ? a.v : a.k;
-    const long long at = h * st.h + t * st.n + 8 * piece;
-    store4<E, VEC>(dst, at, x0);
-    store4<E, VEC>(dst, at + 4, x1);
+    if (a.v && x.t0 + x.jv < a.T) {
+        float v[4][CV] = {};
+        if (x.there_v) {
+            const uint8_t* page = a.store + ((long long)(x.slot_v / kPage) * a.H + x.h) * L::bytes;
+            const int tok = x.slot_v % kPage;
+            const bool nan = page[L::ks + k_scale_at<D>(tok, 0)] == 255;
+            const uint8_t* from = page + L::v + ((tok >> 3) * 32 * 8 + (tok & 7)) * (D / 64) + x.r * (D / 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t byte = page[L::vs + ((tok >> 3) * GROUPS + (D == 128 ? i : i >> 1)) * 8 + (tok & 7)];
+                uint32_t c;
+                if constexpr (D == 128) c = *reinterpret_cast<const uint16_t*>(from + 8 * i * (D / 8));
+                else c = from[8 * i * (D / 8)];
+                decode<CV>(c, __uint_as_float(byte << 23), v[i]);
+                if (nan) {
+#pragma unroll
+                    for (int y = 0; y < CV; ++y) v[i][y] = not_a_number;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_run<E, VEC>(a.v, x.h * a.sv.h + (x.t0 + x.jv) * a.sv.n + CV * (x.r + 8 * i), v[i]);
+    }
 }
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -438,7 +576,7 @@ hipError_t launch_qk_norm_rope(const RopeArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_cache_tables(const TablesArgs& a, hipStream_t st) {
-    const int grid = std::max(1, (int)(((long long)a.rows + kTablesRows - 1) / kTablesRows));
+    const int parts = (int)(((long long)a.rows + kTablesRows - 1) / kTablesRows), grid = parts > 1 ? parts + 1 : 1;
     cache_tables_kernel<<<grid, kTablesThreads, 0, st>>>(a);
     return hipGetLastError();
 }
@@ -446,7 +584,7 @@ hipError_t launch_cache_tables(const TablesArgs& a, hipStream_t st) {
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st) {
     const int size = a.dtype == 0 ? 2 : 4;
     const bool vec = aligned(a.k) && aligned(a.v) && aligned(a.sk, size) && aligned(a.sv, size);
-    const unsigned grid = (unsigned)(((long long)a.T * a.H * (a.d / 4) + 255) / 256);
+    const unsigned grid = (unsigned)(((long long)((a.T + 7) / 8) * a.H + 3) / 4);   // a wave for eight tokens of a head
 #define SOL_APPEND(E, D)                                               \
     do {                                                               \
         if (vec) cache_append_kernel<E, D, true><<<grid, 256, 0, st>>>(a);      \
@@ -466,7 +604,7 @@ hipError_t launch_cache_append(const AppendArgs& a, hipStream_t st) {
 hipError_t launch_cache_read(const ReadArgs& a, hipStream_t st) {
     const int size = a.dtype == 0 ? 2 : 4;
     const bool vec = aligned(a.k) && aligned(a.v) && (!a.k || aligned(a.sk, size)) && (!a.v || aligned(a.sv, size));
-    const unsigned grid = (unsigned)(((long long)a.T * a.H * (a.d / 4) + 255) / 256);
+    const unsigned grid = (unsigned)(((long long)((a.T + 7) / 8) * a.H + 3) / 4);   // a wave for eight tokens of a head
 #define SOL_READ(E, D)                                                 \
     do {                                                               \
         if (vec) cache_read_kernel<E, D, true><<<grid, 256, 0, st>>>(a);        \
