@@ -127,9 +127,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const RopeArgs a, con
         f32x4 w0, w1;
         weights(w, w0, w1);
         const long long xi = b * sx.b + n * sx.n, yi = b * sy.b + n * sy.n;
-#pragma unroll 2
+        f32x4 next0 = load4<E, VEC>(x, xi + lo * sx.h + c0), next1 = load4<E, VEC>(x, xi + lo * sx.h + c1);
         for (int h = lo; h < hi; ++h) {
-            f32x4 x0 = load4<E, VEC>(x, xi + h * sx.h + c0), x1 = load4<E, VEC>(x, xi + h * sx.h + c1);
+            f32x4 x0 = next0, x1 = next1;
+            if (h + 1 < hi) {
+                next0 = load4<E, VEC>(x, xi + (h + 1) * sx.h + c0);
+                next1 = load4<E, VEC>(x, xi + (h + 1) * sx.h + c1);
+            }
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) ss += x0[i] * x0[i] + x1[i] * x1[i];
@@ -175,7 +179,8 @@ __device__ __forceinline__ int upper_bound(const int* sum, int n, int x) {
 }
 
 __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const TablesArgs a) {
-    __shared__ int s_rows[kMaxRequests], s_need[kMaxRequests], s_gone[kMaxRequests];   // inclusive sums
+    __shared__ int s_rows_need[2 * kMaxRequests], s_gone[kMaxRequests];               // inclusive sums
+    int *const s_rows = s_rows_need, *const s_need = s_rows_need + kMaxRequests;
     __shared__ int s_len[kMaxRequests];                                                // held length; ~length: refused
     __shared__ long long w_rows[16];
     __shared__ int w_need[16], w_gone[16], s_taken;
@@ -240,7 +245,9 @@ __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const Tabl
     __syncthreads();
     const int taken = s_taken;
     auto held = [&](int s) { return s_len[s] < 0 ? ~s_len[s] : s_len[s]; };
-    auto fresh = [&](int rank) { return a.ring[(int)(((long long)head + rank) % P)]; };
+    // places of the ring: head < P, and ranks up to P
+    auto place = [&](int at) { return at >= P ? at - P : at; };
+    auto fresh = [&](int rank) { return a.ring[place(head + rank)]; };
     for (int r = blockIdx.x * kTablesThreads + tid; r < taken; r += gridDim.x * kTablesThreads) {
         const int s = upper_bound(s_need, S, r);
         const int page = (held(s) + kPage - 1) / kPage + r - (s ? s_need[s - 1] : 0);
@@ -265,20 +272,42 @@ __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const Tabl
         a.positions[t] = pos;
     }
     if (blockIdx.x) return;
-    // Pages that come back, in order: the valid ones of 8,192 entries at a time, eight to a thread.
+    // Pages that come back, in order: the valid ones of 8,192 entries at a time, eight to a thread.  Every request marks the first of
+    // its entries with its number; the largest mark up to an entry is the number of its request.
+    constexpr int kGone = 2 * kMaxRequests;
+    static_assert(kGone == 8 * kTablesThreads, "eight entries to a thread");
     const int total_gone = s_gone[S - 1];
+    int* const mark = s_rows_need;
     int base = 0;
-    for (int r0 = 0; r0 < total_gone; r0 += 8 * kTablesThreads) {
+    for (int r0 = 0; r0 < total_gone; r0 += kGone) {
+        __syncthreads();   // the sums, and the marks and counts of the round before, have been read
+        for (int i = tid; i < kGone; i += kTablesThreads) mark[i] = 0;
+        __syncthreads();
+        for (int s = e0; s < e1; ++s) {
+            const int first = s ? s_gone[s - 1] : 0, end = s_gone[s];
+            if (first < end && end > r0 && first < r0 + kGone) mark[max(first - r0, 0)] = s + 1;
+        }
+        __syncthreads();
         const int first = r0 + 8 * tid;
-        int page[8], valid = 0;
-        int s = first < total_gone ? upper_bound(s_gone, S, first) : 0;
+        int owner[8], page[8], valid = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) owner[i] = i ? max(owner[i - 1], mark[8 * tid + i]) : mark[8 * tid];
+        int before = owner[7];
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const int x = __shfl_up(before, m);
+            if (lane >= m) before = max(before, x);
+        }
+        if (lane == 63) w_gone[wave] = before;
+        before = __shfl_up(before, 1);
+        if (lane == 0) before = 0;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) before = max(before, w_gone[w]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            const int s = max(owner[i], before) - 1;
             page[i] = -1;
-            if (first + i < total_gone) {
-                while (s_gone[s] <= first + i) ++s;
-                page[i] = a.table[(long long)s * MP + (held(s) + kPage - 1) / kPage - (s_gone[s] - first - i)];
-            }
+            if (first + i < total_gone) page[i] = a.table[(long long)s * MP + (held(s) + kPage - 1) / kPage - (s_gone[s] - first - i)];
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) valid += page[i] >= 0 && page[i] < P;
@@ -288,7 +317,6 @@ __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const Tabl
             const int x = __shfl_up(upto, m);
             if (lane >= m) upto += x;
         }
-        __syncthreads();
         if (lane == 63) w_need[wave] = upto;
         __syncthreads();
         int rank = base + upto - valid;
@@ -299,12 +327,12 @@ __global__ __launch_bounds__(kTablesThreads) void cache_tables_kernel(const Tabl
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (page[i] < 0 || page[i] >= P) continue;
-            if (rank < P - count) a.ring[(int)(((long long)head + count + rank) % P)] = page[i];
+            if (rank < P - count) a.ring[place(place(head + count) + rank)] = page[i];
             ++rank;
         }
     }
     if (tid == 0) {
-        a.state_out[0] = (int)(((long long)head + taken) % P);
+        a.state_out[0] = place(head + taken);
         a.state_out[1] = count - taken + min(base, P - count);
     }
 }
