@@ -13,7 +13,6 @@ contiguous: pass the projection's output through ``transpose`` and it is read wh
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 from typing import NamedTuple, Optional
@@ -55,17 +54,20 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-_here = contextlib.nullcontext()
-
-
-def _on(device):
-    """The library launches on the current device: makes it the tensors' one for the call."""
-    if device.index is None or torch.cuda.current_device() == device.index:
-        return _here
-    return torch.cuda.device(device)
+def _call(fn, device, *args):
+    """One call of the library on the tensors' device and its current stream.  The library launches on the current device:
+    another one is made current for the call."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        rc = fn(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream(device))
+    if rc != _b.SOL_OK:
+        raise _b.SolAttnError(rc, _b.last_error())
 
 
 _DTYPES = {torch.bfloat16: _b.SOL_BF16, torch.float32: _b.SOL_F32}
+_F32_ONLY = (torch.float32,)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -73,6 +75,10 @@ def _stride_array(shape, stride):
     """Strides of all dimensions but the last, as a C array (of a dimension of one element: 0)."""
     s = [st if n > 1 else 0 for st, n in zip(stride[:-1], shape[:-1])]
     return (ctypes.c_longlong * len(s))(*s)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _strides(t):
@@ -90,7 +96,9 @@ def _stream(device) -> int:
 
 
 def _check_heads(name, t, dim, ref=None, writable=False):
-    if t.dim() == dim and t.is_contiguous() and t.dtype in _DTYPES and (ref is None or (t.dtype is ref.dtype and t.device == ref.device)):
+    # the common case first: these checks are a good part of what a short call costs
+    if t.dim() == dim and t.stride(-1) == 1 and t.dtype in _DTYPES and not writable and \
+            (ref is None or (t.dtype is ref.dtype and t.device == ref.device)):
         return
     if t.dim() != dim:
         raise ValueError(f"{name} must have {dim} dimensions (got {tuple(t.shape)})")
@@ -109,6 +117,12 @@ def _check_heads(name, t, dim, ref=None, writable=False):
             if st < reach:
                 raise ValueError(f"rows of {name} overlap")
             reach = st * (n - 1) + reach
+
+
+def _check_floats(name, t, shape, dtypes, device):
+    if t.dtype in dtypes and t.shape == shape and t.device == device and t.is_contiguous():
+        return
+    _b._check_buffer(name, t, shape, dtypes, device)
 
 
 def _check_ints(name, t, shape, device):
@@ -159,7 +173,7 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, positio
         if w is not None:
             if x is None:
                 raise ValueError(f"{name} needs {name[0]}")
-            _b._check_buffer(name, w, (d,), (torch.bfloat16, torch.float32), device)
+            _check_floats(name, w, (d,), _DTYPES, device)
             if wdtype is not None and w.dtype != wdtype:
                 raise ValueError("q_weight and k_weight must have one dtype")
             wdtype = w.dtype
@@ -170,8 +184,8 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, positio
         if cos.dim() != 2:
             raise ValueError("cos and sin must be [P, rot / 2]")
         P, rot = cos.shape[0], 2 * cos.shape[1]
-        _b._check_buffer("cos", cos, cos.shape, (torch.float32,), device)
-        _b._check_buffer("sin", sin, cos.shape, (torch.float32,), device)
+        _check_floats("cos", cos, cos.shape, _F32_ONLY, device)
+        _check_floats("sin", sin, cos.shape, _F32_ONLY, device)
     if positions is not None:
         _check_ints("positions", positions, (B, N), device)
     if q_out is not None or k_out is not None:
@@ -187,15 +201,13 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, positio
         _disjoint("q_out", q_out, k_out=k_out)
     _b._require_gpu(ref)
     if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=device)
-    with _on(device):
-        _b._check(lib().sol_qk_norm_rope(
-            _b._ptr(q), _b._ptr(k), _b._ptr(q_out), _b._ptr(k_out), _strides(q), _strides(k), _strides(q_out), _strides(k_out),
-            _b._ptr(q_weight), _b._ptr(k_weight), _b._ptr(cos), _b._ptr(sin), _b._ptr(positions), B,
-            0 if q is None else q.shape[1], 0 if k is None else k.shape[1], N, d, P, rot, PAIRS if interleaved else HALVES, eps,
-            _DTYPES[ref.dtype], _b.SOL_F32 if wdtype is torch.float32 else _b.SOL_BF16, _stream(device)))
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+    _call(lib().sol_qk_norm_rope, device, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _strides(q), _strides(k), _strides(q_out),
+          _strides(k_out), _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin), _ptr(positions), B,
+          0 if q is None else q.shape[1], 0 if k is None else k.shape[1], N, d, P, rot, PAIRS if interleaved else HALVES, eps,
+          _DTYPES[ref.dtype], _b.SOL_F32 if wdtype is torch.float32 else _b.SOL_BF16)
     return q_out, k_out
 
 
@@ -233,12 +245,10 @@ def tables(lens, add, table, ring, state, rows: int, out: Optional[Step] = None)
                       **{f"out.{o}": getattr(out, o) for o in shapes if o != name})
     _b._require_gpu(lens)
     if out is None:
-        sizes = (S + 1, rows, rows, S, 2)
-        out = Step(*torch.empty(S + 1 + 2 * rows + S + 2, dtype=torch.int32, device=device).split(sizes))
-    with _on(device):
-        _b._check(lib().sol_cache_tables(lens.data_ptr(), add.data_ptr(), table.data_ptr(), ring.data_ptr(), state.data_ptr(),
-                                         out[3].data_ptr(), out[4].data_ptr(), out[0].data_ptr(), out[1].data_ptr(),
-                                         out[2].data_ptr(), S, MP, ring.shape[0], rows, _stream(device)))
+        flat = torch.empty(S + 1 + 2 * rows + S + 2, dtype=torch.int32, device=device)
+        out = Step(*torch.split_with_sizes(flat, (S + 1, rows, rows, S, 2)))
+    _call(lib().sol_cache_tables, device, lens.data_ptr(), add.data_ptr(), table.data_ptr(), ring.data_ptr(), state.data_ptr(),
+          out[3].data_ptr(), out[4].data_ptr(), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), S, MP, ring.shape[0], rows)
     return out
 
 
@@ -281,9 +291,8 @@ def append(k, v, store, slots):
     T = k.shape[1]
     _check_ints("slots", slots, (T,), device)
     _b._require_gpu(k)
-    with _on(device):
-        _b._check(lib().sol_cache_append(k.data_ptr(), v.data_ptr(), _strides(k), _strides(v), store.data_ptr(), slots.data_ptr(),
-                                         T, H, d, P, _DTYPES[k.dtype], _stream(device)))
+    _call(lib().sol_cache_append, device, k.data_ptr(), v.data_ptr(), _strides(k), _strides(v), store.data_ptr(), slots.data_ptr(),
+          T, H, d, P, _DTYPES[k.dtype])
 
 
 def read(store, slots, dtype=None, k_out=None, v_out=None):
@@ -316,9 +325,8 @@ def read(store, slots, dtype=None, k_out=None, v_out=None):
     if not given:
         k_out = torch.empty((H, T, d), dtype=dt, device=device)
         v_out = torch.empty((H, T, d), dtype=dt, device=device)
-    with _on(device):
-        _b._check(lib().sol_cache_read(store.data_ptr(), slots.data_ptr(), _b._ptr(k_out), _b._ptr(v_out), _strides(k_out),
-                                       _strides(v_out), T, H, d, P, _DTYPES[dt], _stream(device)))
+    _call(lib().sol_cache_read, device, store.data_ptr(), slots.data_ptr(), _ptr(k_out), _ptr(v_out), _strides(k_out),
+          _strides(v_out), T, H, d, P, _DTYPES[dt])
     return k_out, v_out
 
 
@@ -372,14 +380,14 @@ def forward(q, store, table, lens, row_start, positions, causal_granule: int = 1
         need = call.sol_cache_workspace_bytes(S, T, rows, Hq, Hk, d, MP)
         if need and need != _INVALID:   # invalid arguments are the call's to report
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    given = out is not None or not _dense(q.shape, q.stride())   # whether out's strides may be others than q's
     if out is None:
-        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=device) if _dense(q.shape, q.stride()) else \
-            torch.empty(q.shape, dtype=q.dtype, device=device)
-    with _on(device):
-        _b._check(call.sol_cache_forward(
-            q.data_ptr(), _strides(q), out.data_ptr(), _strides(out), store.data_ptr(), table.data_ptr(), lens.data_ptr(),
-            row_start.data_ptr(), positions.data_ptr(), S, T, rows, Hq, Hk, d, P, MP, causal_granule, _DTYPES[q.dtype],
-            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream(device)))
+        out = torch.empty(q.shape, dtype=q.dtype, device=device) if given else torch.empty_like(q)
+    strides = _strides(q)
+    _call(call.sol_cache_forward, device, q.data_ptr(), strides, out.data_ptr(), _strides(out) if given else strides,
+          store.data_ptr(), table.data_ptr(), lens.data_ptr(), row_start.data_ptr(), positions.data_ptr(), S, T, rows, Hq, Hk, d, P,
+          MP, causal_granule, _DTYPES[q.dtype], None if workspace is None else workspace.data_ptr(),
+          0 if workspace is None else workspace.numel())
     return out
 
 
