@@ -37,6 +37,7 @@ SIGNATURES = {
     "sol_cache_forward": (_I, [_P, _L, _P, _L] + [_P] * 5 + [_I] * 10 + [_P, _S, _P]),
 }
 _INVALID = ctypes.c_size_t(-1).value
+_INT_MAX = 2 ** 31 - 1
 
 _lib = None
 
@@ -200,10 +201,14 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, positio
             _disjoint(name, out, q=q, k=k, cos=cos, sin=sin, positions=positions, q_weight=q_weight, k_weight=k_weight)
         _disjoint("q_out", q_out, k_out=k_out)
     _b._require_gpu(ref)
+    if P > _INT_MAX or rot > _INT_MAX:
+        raise ValueError("cos and sin are too large")
     if q is not None and q_out is None:
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if k is not None and k_out is None:
         k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+    if B == 0 or N == 0:
+        return q_out, k_out
     _call(lib().sol_qk_norm_rope, device, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _strides(q), _strides(k), _strides(q_out),
           _strides(k_out), _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin), _ptr(positions), B,
           0 if q is None else q.shape[1], 0 if k is None else k.shape[1], N, d, P, rot, PAIRS if interleaved else HALVES, eps,
@@ -234,8 +239,8 @@ def tables(lens, add, table, ring, state, rows: int, out: Optional[Step] = None)
     _check_ints("table", table, (S, MP), device)
     _check_ints("ring", ring, ring.shape, device)
     _check_ints("state", state, (2,), device)
-    if rows < 0:
-        raise ValueError(f"rows must not be negative (got {rows})")
+    if not 0 <= rows <= 1 << 30:
+        raise ValueError(f"rows must be from 0 to 2^30 (got {rows})")
     if out is not None:
         shapes = {"row_start": (S + 1,), "slots": (rows,), "positions": (rows,), "lens": (S,), "state": (2,)}
         for name, shape in shapes.items():
@@ -291,6 +296,8 @@ def append(k, v, store, slots):
     T = k.shape[1]
     _check_ints("slots", slots, (T,), device)
     _b._require_gpu(k)
+    if T == 0:
+        return
     _call(lib().sol_cache_append, device, k.data_ptr(), v.data_ptr(), _strides(k), _strides(v), store.data_ptr(), slots.data_ptr(),
           T, H, d, P, _DTYPES[k.dtype])
 
@@ -325,6 +332,8 @@ def read(store, slots, dtype=None, k_out=None, v_out=None):
     if not given:
         k_out = torch.empty((H, T, d), dtype=dt, device=device)
         v_out = torch.empty((H, T, d), dtype=dt, device=device)
+    if T == 0:
+        return k_out, v_out
     _call(lib().sol_cache_read, device, store.data_ptr(), slots.data_ptr(), _ptr(k_out), _ptr(v_out), _strides(k_out),
           _strides(v_out), T, H, d, P, _DTYPES[dt])
     return k_out, v_out
@@ -374,19 +383,22 @@ def forward(q, store, table, lens, row_start, positions, causal_granule: int = 1
         _b._check_buffer("workspace", workspace, workspace.shape, (torch.uint8,), q.device)
         _disjoint("workspace", workspace, q=q, store=store, table=table, lens=lens, row_start=row_start, positions=positions)
     _b._require_gpu(q)
-    rows = T if max_rows is None else int(max_rows)
+    rows = T if max_rows is None else min(int(max_rows), T)
+    granule = min(int(causal_granule), _INT_MAX)   # longer than any sequence
     call = lib()
-    if workspace is None:
+    if workspace is None and T > 0:
         need = call.sol_cache_workspace_bytes(S, T, rows, Hq, Hk, d, MP)
         if need and need != _INVALID:   # invalid arguments are the call's to report
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
     given = out is not None or not _dense(q.shape, q.stride())   # whether out's strides may be others than q's
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=device) if given else torch.empty_like(q)
+    if T == 0:
+        return out
     strides = _strides(q)
     _call(call.sol_cache_forward, device, q.data_ptr(), strides, out.data_ptr(), _strides(out) if given else strides,
           store.data_ptr(), table.data_ptr(), lens.data_ptr(), row_start.data_ptr(), positions.data_ptr(), S, T, rows, Hq, Hk, d, P,
-          MP, causal_granule, _DTYPES[q.dtype], None if workspace is None else workspace.data_ptr(),
+          MP, granule, _DTYPES[q.dtype], None if workspace is None else workspace.data_ptr(),
           0 if workspace is None else workspace.numel())
     return out
 

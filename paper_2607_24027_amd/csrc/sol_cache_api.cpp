@@ -67,7 +67,7 @@ int sol_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, con
         return fail(SOL_ERR_INVALID_ARG, "weight_dtype must be SOL_BF16 or SOL_F32 (got %d)", weight_dtype);
     if (B <= 0 || N <= 0 || Hq < 0 || Hk < 0 || Hq + (long long)Hk == 0)
         return fail(SOL_ERR_INVALID_ARG, "B, N and the heads must be positive (got %d, %d, %d, %d)", B, N, Hq, Hk);
-    if (Hq + (long long)Hk > 65535 || (long long)B * N > (1LL << 34))
+    if (Hq + (long long)Hk > 65535 || (long long)B * N > (1LL << 27))
         return fail(SOL_ERR_UNSUPPORTED, "too many heads or tokens (got %lld, %lld)", Hq + (long long)Hk, (long long)B * N);
     if (!q != (Hq == 0) || !k != (Hk == 0) || !q != !q_out || !k != !k_out)
         return fail(SOL_ERR_INVALID_ARG, "q and k need heads and an output each, or neither");
@@ -118,7 +118,7 @@ int sol_cache_append(const void* k, const void* v, const long long* k_strides, c
     SOL_CHECK(check_head(d, dtype));
     SOL_CHECK(check_store(store, heads, P));
     if (T <= 0) return fail(SOL_ERR_INVALID_ARG, "T must be positive (got %d)", T);
-    if ((long long)T * heads > (1LL << 34)) return fail(SOL_ERR_UNSUPPORTED, "too many tokens and heads");
+    if ((long long)T * heads > (1LL << 28)) return fail(SOL_ERR_UNSUPPORTED, "too many tokens and heads (got %d, %d)", T, heads);
     SOL_CHECK(check_strides("k", k_strides, 2));
     SOL_CHECK(check_strides("v", v_strides, 2));
     sol::AppendArgs a{k, v, two(k_strides), two(v_strides), static_cast<uint8_t*>(store), slots, T, heads, d, P, dtype};
@@ -131,7 +131,7 @@ int sol_cache_read(const void* store, const int32_t* slots, void* k_out, void* v
     SOL_CHECK(check_head(d, dtype));
     SOL_CHECK(check_store(store, heads, P));
     if (T <= 0) return fail(SOL_ERR_INVALID_ARG, "T must be positive (got %d)", T);
-    if ((long long)T * heads > (1LL << 34)) return fail(SOL_ERR_UNSUPPORTED, "too many tokens and heads");
+    if ((long long)T * heads > (1LL << 28)) return fail(SOL_ERR_UNSUPPORTED, "too many tokens and heads (got %d, %d)", T, heads);
     if (k_out == v_out) return fail(SOL_ERR_INVALID_ARG, "k_out and v_out must differ");
     if (k_out) SOL_CHECK(check_strides("k_out", k_strides, 2));
     if (v_out) SOL_CHECK(check_strides("v_out", v_strides, 2));
@@ -153,7 +153,9 @@ static int check_attn(int S, int T, int max_rows, int Hq, int Hk, int d, int max
     if (d != 64 && d != 128) return fail(SOL_ERR_UNSUPPORTED, "d must be 64 or 128 (got %d)", d);
     if (S > sol::kMaxRequests) return fail(SOL_ERR_UNSUPPORTED, "at most %d requests (got %d)", sol::kMaxRequests, S);
     if (max_pages > (1 << 24) || (long long)S * max_pages > (1LL << 30)) return fail(SOL_ERR_UNSUPPORTED, "too many table entries");
-    if (Hq > 65535 || (long long)T * Hq > (1LL << 28)) return fail(SOL_ERR_UNSUPPORTED, "too many query rows (got %d tokens of %d heads)", T, Hq);
+    // launches of fewer than 2^32 threads
+    if (Hq > 65535 || (long long)T * Hq > (1LL << 24) || (long long)S * Hk > (1LL << 18))
+        return fail(SOL_ERR_UNSUPPORTED, "too many query rows or requests (got %d tokens of %d heads, %d requests of %d)", T, Hq, S, Hk);
     return SOL_OK;
 }
 

@@ -41,8 +41,8 @@ constexpr int kManyWaves = 4;                    // waves of a workgroup of cach
 constexpr int kFewTile = 16, kManyTile = 32 * kManyWaves;   // query rows of a piece
 constexpr int kFewRows = 48;                    // a request of more goes to cache_many_kernel
 constexpr int kFewSlots = 3072;                 // waves of cache_few_kernel that the GPU holds, 12 a compute unit
-constexpr int kManySlots = 2048 / kManyWaves;                 // workgroups of cache_many_kernel that it holds, two a compute unit
-constexpr int kRounds = 7;                      // fillings of those slots at most
+constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (three at d = 64 are slower)
+constexpr int kRounds = 7;                      // fillings of those slots at most (below 8: a lane for each of eight requests)
 constexpr int kFewCost = 2, kManyCost = 8;      // what starting a piece and joining its result costs, in pages
 constexpr int kLeastPages = 2;                  // least pages of a piece
 constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
@@ -140,14 +140,35 @@ __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& pa
     int per = pages_for(sum, tiles, part.slots, a.S > 64 ? 2 : 1);
     if (a.S <= 64 && tiles > 0.5f * (float)part.slots) {
         if (planned) return *planned;
-        const float mine = (float)r.tiles * (float)a.Hk, pages = (float)r.pages;
+        const float heads = (float)a.Hk;
+        auto cost_of = [&](float pieces, float longest) {
+            return (sum + pieces * (float)part.cost) / (float)part.slots + 0.5f * (longest + (float)part.cost);
+        };
         float least = INFINITY;
-        for (int k = 1; k <= kRounds; ++k) {
-            const int p = pages_for(sum, tiles, part.slots, k);
+        if (a.S <= 8) {   // lane 8 (k - 1) + s: all k at once (1.5 us less than one after the other)
+            const float t = (float)__shfl(r.tiles, lane & 7), pages = (float)__shfl(r.pages, lane & 7);
+            const int p = pages_for(sum, tiles, part.slots, (lane >> 3) + 1);
             const float chunks = fmaxf(ceilf(pages / (float)p), 1.f);
-            const float pieces = at_lane(scan_add(mine * chunks), 63), longest = wave_max(r.tiles ? pages / chunks : 0.f);
-            const float cost = (sum + pieces * (float)part.cost) / (float)part.slots + 0.5f * (longest + (float)part.cost);
-            if (cost < least) least = cost, per = p;
+            float pieces = t * chunks * heads, longest = t > 0.f ? pages / chunks : 0.f;
+#pragma unroll
+            for (int m = 1; m < 8; m *= 2) {
+                pieces += __shfl_xor(pieces, m);
+                longest = fmaxf(longest, __shfl_xor(longest, m));
+            }
+            const float cost = cost_of(pieces, longest);
+#pragma unroll
+            for (int k = 0; k < kRounds; ++k) {
+                const float c = at_lane(cost, 8 * k);
+                if (c < least) least = c, per = at_lane(p, 8 * k);
+            }
+        } else {
+            for (int k = 1; k <= kRounds; ++k) {
+                const int p = pages_for(sum, tiles, part.slots, k);
+                const float pages = (float)r.pages, chunks = fmaxf(ceilf(pages / (float)p), 1.f);
+                const float pieces = at_lane(scan_add((float)r.tiles * chunks * heads), 63), longest = wave_max(r.tiles ? pages / chunks : 0.f);
+                const float cost = cost_of(pieces, longest);
+                if (cost < least) least = cost, per = p;
+            }
         }
     }
     return per;
@@ -403,6 +424,13 @@ struct Pages {
         there = __ballot(entry >= 0 && entry < P);
     }
     __device__ __forceinline__ Pages(const int* t, int P_, int p0, int p1) : table(t), P(P_), end(p1), base(p0), there(0), entry(-1), p(p0) { fill(); }
+    // Leaves out pages from `to` on; whether the one that next() found stays.
+    __device__ __forceinline__ bool limit(int to) {
+        end = min(end, to);
+        const int n = end - base;
+        if (n < 64) there &= n > 0 ? (1ull << n) - 1 : 0;
+        return p < end;
+    }
     // The next page's place in the store, or -1.
     __device__ __forceinline__ int next() {
         while (!there) {
@@ -593,33 +621,10 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
     if (blockIdx.x == 0 && ws && lane == 0) ws->per = per;
     if (!find_piece<false>(a, part, per, request_of_lane, blockIdx.x, false, pc)) return;
 
-    const int r = pc.tile * kFewTile + j;
-    const bool valid = r < pc.rows;
-    const int token = pc.row0 + (valid ? r / G : 0), head = pc.hk * G + (valid ? r % G : 0);
-    const int sees = row_limit(a, token, pc.len);
-    float x[32];
-    if (D == 128 || g < 2) {
-        load_row<F32T, VEC>(a.q, head * a.sq.h + token * a.sq.n + 32 * g, x);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] = 0.f;
-    }
-    int last = sees, least = sees;
-#pragma unroll
-    for (int m = 1; m < 16; m *= 2) {
-        last = max(last, __shfl_xor(last, m));
-        least = min(least, __shfl_xor(least, m));
-    }
-    last = __builtin_amdgcn_readfirstlane(last);
-    least = __builtin_amdgcn_readfirstlane(least);
-    Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, min(pc.p1, (last + kPage - 1) / kPage));
+    // memory is asked for the first page, the rows' positions and the rows at once
     const long long page_stride = (long long)a.Hk * L::bytes;
     const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
-
-    f32x4 o[CT], s[4];
-#pragma unroll
-    for (int t = 0; t < CT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = 0.f, most = -INFINITY, l = 0.f;
+    Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, pc.p1);
     FewPage<D> pg;
     const FewOffsets at = few_offsets<D>();
     int id = pages.next();
@@ -628,6 +633,31 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
         few_load_k<D>(page, at, pg);
         few_load_v<D>(page, at, pg);
     }
+    const int r = pc.tile * kFewTile + j;
+    const bool valid = r < pc.rows;
+    const int token = pc.row0 + (valid ? r / G : 0), head = pc.hk * G + (valid ? r % G : 0);
+    float x[32];
+    if (D == 128 || g < 2) {
+        load_row<F32T, VEC>(a.q, head * a.sq.h + token * a.sq.n + 32 * g, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = 0.f;
+    }
+    const int sees = row_limit(a, token, pc.len);
+    int last = sees, least = sees;
+#pragma unroll
+    for (int m = 1; m < 16; m *= 2) {
+        last = max(last, __shfl_xor(last, m));
+        least = min(least, __shfl_xor(least, m));
+    }
+    last = __builtin_amdgcn_readfirstlane(last);
+    least = __builtin_amdgcn_readfirstlane(least);
+    if (!pages.limit((last + kPage - 1) / kPage)) id = -1;
+
+    f32x4 o[CT], s[4];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = 0.f, most = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] *= scale_log2;
     const Split<NT> q = split_row<NT>(x);
@@ -819,7 +849,7 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64 * kManyWaves, 8 / kManyWaves * (kManyWaves / 4)) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
+__global__ __launch_bounds__(64 * kManyWaves, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
                                                                                                        PartSpace* ws) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
@@ -831,6 +861,14 @@ __global__ __launch_bounds__(64 * kManyWaves, 8 / kManyWaves * (kManyWaves / 4))
     if (!find_piece_shared<false>(a, part, ws, blockIdx.x, true, pc)) return;
     const unsigned slot = pc.slot0 + (unsigned)pc.chunk * pc.tiles;
 
+    // memory is asked for the first page, the rows' positions and the rows at once
+    constexpr int N = kManyWaves / 4;
+    const long long page_stride = (long long)a.Hk * L::bytes;
+    const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
+    Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, pc.p1);
+    ManyPage<D, N> pg;
+    int id = pages.next();
+    if (id >= 0) many_load<D, N>(store + id * page_stride, pg);
     const int r = pc.tile * kManyTile + 32 * wave + j;
     const bool valid = r < pc.rows;
     const int token = pc.row0 + (valid ? r / G : 0), head = pc.hk * G + (valid ? r % G : 0);
@@ -858,9 +896,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 8 / kManyWaves * (kManyWaves / 4))
     int all = 0;
 #pragma unroll
     for (int w = 0; w < kManyWaves; ++w) all = max(all, s_last[w]);
-    Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, __builtin_amdgcn_readfirstlane(min(pc.p1, (all + kPage - 1) / kPage)));
-    const long long page_stride = (long long)a.Hk * L::bytes;
-    const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
+    bool more = pages.limit(__builtin_amdgcn_readfirstlane((all + kPage - 1) / kPage)) && id >= 0;
 
     f32x16 o[CT], off;
 #pragma unroll
@@ -872,12 +908,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 8 / kManyWaves * (kManyWaves / 4))
     for (int i = 0; i < 16; ++i) off[i] = kShift;
 
     // the page of tokens key0 ... is in stage[turn], the one after it in registers
-    constexpr int N = kManyWaves / 4;
-    ManyPage<D, N> pg;
-    int id = pages.next(), turn = 0, key0 = pages.p * kPage;
-    bool more = id >= 0;
+    int turn = 0, key0 = pages.p * kPage;
     if (more) {
-        many_load<D, N>(store + id * page_stride, pg);
         many_store<D, N>(pg, stage[0], pc.len - key0);
         id = pages.next();
         if (id >= 0) many_load<D, N>(store + id * page_stride, pg);
@@ -923,26 +955,38 @@ __global__ __launch_bounds__(64 * kManyWaves, 8 / kManyWaves * (kManyWaves / 4))
 }
 
 // ---------------------------------------------------------------------------
-// Joins the shares of a tile's rows (gridDim.y workgroups a tile, of the few for four rows each), in an order that the plan fixes.  D / 4 threads hold a row, four
+// Joins the shares of a tile's rows, of both kernels' pieces in one launch, in an order that the plan fixes.  D / 4 threads hold a row, four
 // channels each; where there are fewer rows than groups, the shares are dealt to several groups, whose sums are added in LDS.  Bound
 // by latency: the plan, the maxima, the sums.
 // ---------------------------------------------------------------------------
 constexpr int kJoinThreads = 512;
 
+struct JoinPart {
+    Part part;
+    PartSpace* ws;
+    unsigned pieces, tiles, per_tile;   // per_tile workgroups a tile, for `rows` rows each
+    int rows;
+};
+
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttnArgs a, const Part part, const unsigned pieces, PartSpace* ws) {
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttnArgs a, const JoinPart first_part, const JoinPart second_part) {
     constexpr int LANES = D / 4, GROUPS = kJoinThreads / LANES;
     __shared__ f32x4 s_o[GROUPS][LANES];
     __shared__ float s_l[GROUPS];
     const int G = a.Hq / a.Hk;
+    const unsigned head = first_part.tiles * first_part.per_tile;
+    const bool second = blockIdx.x >= head;
+    const JoinPart jp = second ? second_part : first_part;
+    const Part part = jp.part;
+    const unsigned block = blockIdx.x - (second ? head : 0);
     Piece pc;
-    if (!find_piece_shared<true>(a, part, ws, blockIdx.x, false, pc) || pc.chunks == 1) return;
-    if (pc.slot0 + (uint64_t)(pc.chunks - 1) * pc.tiles >= pieces) return;   // rows that overlap: no room was asked for
+    if (!find_piece_shared<true>(a, part, jp.ws, block / jp.per_tile, false, pc) || pc.chunks == 1) return;
+    if (pc.slot0 + (uint64_t)(pc.chunks - 1) * pc.tiles >= jp.pieces) return;   // rows that overlap: no room was asked for
     const long long stride = (long long)pc.tiles * (part.tile * (D + 2));
-    const float* const tile = ws->results + (long long)pc.slot0 * (part.tile * (D + 2));
+    const float* const tile = jp.ws->results + (long long)pc.slot0 * (part.tile * (D + 2));
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    const int each = part.tile == kFewTile ? 4 : part.tile / gridDim.y, row0 = each * blockIdx.y, first = pc.tile * part.tile + row0;
-    const int rows = min(pc.rows - first, each);   // of this workgroup
+    const int row0 = jp.rows * (block % jp.per_tile), first = pc.tile * part.tile + row0;
+    const int rows = min(pc.rows - first, jp.rows);   // of this workgroup
     int width = 1;   // rows at a time, a power of two
     while (width < GROUPS && width < rows) width *= 2;
     const int shares = GROUPS / width, share = group / width;
@@ -1061,12 +1105,10 @@ static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) 
         cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_pieces, 64, 0, st>>>(a, p.few, scale_log2, few_ws);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (p.many_bytes) {
-        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.many_tiles, kManyTile / 32), kJoinThreads, 0, st>>>(a, p.many, (unsigned)p.many_pieces, many_ws);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (p.few_bytes) {
-        cache_join_kernel<D, F32T, VEC><<<dim3((unsigned)p.few_tiles, (unsigned)p.few_quads), kJoinThreads, 0, st>>>(a, p.few, (unsigned)p.few_pieces, few_ws);
+    JoinPart few{p.few, few_ws, (unsigned)p.few_pieces, few_ws ? (unsigned)p.few_tiles : 0u, (unsigned)p.few_quads, 4};
+    JoinPart many{p.many, many_ws, (unsigned)p.many_pieces, many_ws ? (unsigned)p.many_tiles : 0u, kManyTile / 32, 32};
+    if (const unsigned grid = few.tiles * few.per_tile + many.tiles * many.per_tile) {
+        cache_join_kernel<D, F32T, VEC><<<grid, kJoinThreads, 0, st>>>(a, few, many);
         e = hipGetLastError();
     }
     return e;

@@ -215,3 +215,39 @@ def test_reference_tables_by_hand():
     got = ora.tables(got[3], [-7, 64], got[5], got[6], got[4], 64)      # the first gives page 5 back, the second is refused
     assert got[3].tolist() == [59, 65] and got[4].tolist() == [2, 1] and got[6][2] == 5
     assert (got[1] == -1).all() and (got[2] == -1).all()
+
+
+def test_sizes_past_a_launch_are_refused():
+    assert rope(N=(1 << 27) + 1, P=1 << 28) == UNSUPPORTED
+    assert append(T=(1 << 27) + 1) == UNSUPPORTED and read(T=(1 << 27) + 1) == UNSUPPORTED
+    assert attn(T=(1 << 21) + 1, rows=1) == UNSUPPORTED
+    assert attn(S=4096, T=4096, rows=1, Hq=128, Hk=128) == UNSUPPORTED
+
+
+def test_device_of_the_tensors_is_made_current_for_the_call(monkeypatch):
+    calls = []
+
+    class Guard:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            calls.append(("enter", self.device))
+
+        def __exit__(self, *a):
+            calls.append(("exit", self.device))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(sc, "_stream", lambda device: 100 + device.index)
+
+    def fn(*args):
+        calls.append(args)
+        return 0
+    sc._call(fn, torch.device("cuda", 0), 1, 2)
+    assert calls == [(1, 2, 100)]
+    calls.clear()
+    other = torch.device("cuda", 1)
+    sc._call(fn, other, 3)
+    assert calls == [("enter", other), (3, 101), ("exit", other)]
+    with pytest.raises(sb.SolAttnError):
+        sc._call(lambda *a: -1, torch.device("cuda", 0))

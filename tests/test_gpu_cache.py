@@ -468,6 +468,98 @@ def test_forward_many_requests(dev):
     check_forward(dev, "bf16", 64, 2, 1, lens, rows, 1, seed=12)
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_forward_random(dev, seed):
+    """Shapes, lengths, masks and layouts at random; positions that are no run; dropped pages."""
+    rng = np.random.default_rng(1000 + seed)
+    d = int(rng.choice([64, 128]))
+    Hk, G = int(rng.integers(1, 4)), int(rng.choice([1, 2, 3, 4, 7, 16]))
+    S = int(rng.integers(1, 8))
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(900), S))]
+    rows = [int(rng.integers(0, max(2, min(n, 2000 // (S * Hk * G))) + 1)) for n in lens]
+    rows[0] = max(1, rows[0])
+    positions = np.concatenate([rng.integers(-1, n + 3, r) for n, r in zip(lens, rows)])
+    drop = [(s, int(rng.integers(0, -(-n // 64))), int(rng.choice([-1, 1 << 28]))) for s, n in enumerate(lens) if rng.random() < 0.3 and n]
+    granule = int(rng.choice([1, 1, 17, 64, 300, 1 << 30]))
+    check_forward(dev, str(rng.choice(["bf16", "f32"])), d, Hk * G, Hk, lens, rows, granule, str(rng.choice(["plain", "tokens", "odd"])),
+                  seed=seed, positions=positions, drop=drop, extra=0)
+
+
+@pytest.mark.parametrize("dtype,d,Hq,Hk,S,rows,lens,granule", [
+    ("bf16", 128, 32, 16, 1, 700, 5000, 1),            # one request, tiles of 128 rows past half of what the GPU holds, cut
+    ("bf16", 64, 64, 16, 3, 300, 2500, 1 << 30),       # few requests, all fillings looked at at once
+    ("f32", 128, 16, 16, 12, 200, 900, 50),            # more than eight requests, one filling after the other
+    ("bf16", 128, 4, 4, 90, 60, 500, 1),               # more requests than lanes, each of many rows
+    ("f32", 64, 12, 12, 70, 3, 700, 1),                # more requests than lanes, each of few rows
+    ("bf16", 128, 8, 1, 1, 2, 200000, 1),              # one long request
+])
+def test_forward_cut_into_pieces(dev, dtype, d, Hq, Hk, S, rows, lens, granule):
+    """Work of a size that is cut, against attention in 64 bits on the GPU, on the values that read() gives."""
+    g = torch.Generator(device=dev).manual_seed(S + rows)
+    rng = np.random.default_rng(S)
+    length = [int(lens * f) for f in rng.uniform(0.4, 1.0, S)]
+    rows = [min(n, max(1, int(rows * f))) for n, f in zip(length, rng.uniform(0.5, 1.0, S))]
+    held = [-(-n // 64) for n in length]
+    P, T = sum(held) + 1, sum(rows)
+    k, v = (torch.randn(Hk, P * 64, d, generator=g, device=dev) for _ in range(2))
+    store = sc.empty(P, Hk, d, dev)
+    slots = torch.arange(P * 64, dtype=torch.int32, device=dev)
+    sc.append(k, v, store, slots)
+    k, v = (x.double() for x in sc.read(store, slots, dtype=torch.float32))
+    order = torch.randperm(P, generator=g, device=dev).int()
+    table = torch.full((S, max(held) + 3), -1, dtype=torch.int32, device=dev)
+    at = 0
+    for s in range(S):
+        table[s, :held[s]] = order[at:at + held[s]]
+        at += held[s]
+    q = torch.randn(T, Hq, d, generator=g, device=dev).to(DT[dtype]).transpose(0, 1)
+    row_start = np.concatenate([[0], np.cumsum(rows)])
+    positions = torch.cat([torch.arange(n - r, n, dtype=torch.int32, device=dev) for n, r in zip(length, rows)])
+    out = sc.forward(q, store, table, i32(length, dev), i32(row_start, dev), positions, causal_granule=granule)
+    off = norm = 0.0
+    for s in range(S):
+        slot = (order[sum(held[:s]):sum(held[:s + 1]), None].long() * 64 + torch.arange(64, device=dev)).flatten()[:length[s]]
+        r0, r1 = row_start[s], row_start[s + 1]
+        limit = (positions[r0:r1].long() // granule + 1) * granule
+        hidden = torch.arange(length[s], device=dev)[None] >= limit[:, None]
+        for h in range(Hq):
+            kk, vv = k[h // (Hq // Hk), slot], v[h // (Hq // Hk), slot]
+            logits = (q[h, r0:r1].double() @ kk.T.contiguous()) / math.sqrt(d)
+            ref = torch.softmax(logits.masked_fill(hidden, -math.inf), -1) @ vv
+            err = out[h, r0:r1].double() - ref
+            # as in tolerance(), with the largest |v| for sum p |v| and half of sum p |v - out|, and the largest |q| for that of a block
+            top, sum_k = q[h, r0:r1].double().abs().amax(), kk.abs().sum(-1).amax()
+            s_abs = top * sum_k / math.sqrt(d)
+            ds = s_abs * ((2.0 ** -11 if dtype == "bf16" else 2.0 ** -23) / 3.75 + (d + 6) * 2.0 ** -24) + 64 * 2.0 ** -24
+            cut = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) + (length[s] / 16 + 64) * 2.0 ** -24 + length[s] * 2.0 ** -29
+            bound = (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * ref.abs() + (4 * ds + cut) * vv.abs().amax()
+            assert bool((err.abs() <= bound).all()), (s, h, float((err.abs() / bound).max()))
+            off, norm = off + float(err.square().sum()), norm + float(ref.square().sum())
+    # Over all values errors add up by their squares: a rounding to bf16 is at most 2^-8 / sqrt(3) of the values, to f16 an eighth
+    # of that; a logit's, 2^-11 / sqrt(3) of a block's largest channel over 3.75 for each of d channels, comes to less than
+    # that of f16, and a row's sum is over weights whose squares add up alike.  f32: as many terms of 2^-22 and less.
+    assert math.sqrt(off / norm) <= (2.0 ** -8 / math.sqrt(3) * 1.25 if dtype == "bf16" else 2.0 ** -20)
+
+
+def test_empty_calls(dev):
+    """No rows at all, and a granule past an int."""
+    rng = np.random.default_rng(3)
+    store, _, _ = make_store(rng, 2, 2, 64, dev)
+    none = torch.empty(0, dtype=torch.int32, device=dev)
+    q = torch.empty(4, 0, 64, device=dev)
+    assert sc.forward(q, store, i32([[0, 1]], dev), i32([100], dev), i32([0, 0], dev), none).shape == (4, 0, 64)
+    before = store.clone()
+    sc.append(q[:2], q[:2], store, none)
+    assert torch.equal(store, before)
+    k, v = sc.read(store, none)
+    assert k.shape == v.shape == (2, 0, 64)
+    y, _ = sc.qk_norm_rope(q[None], None)
+    assert y.shape == (1, 4, 0, 64)
+    q = torch.randn(4, 3, 64, device=dev)
+    args = (store, i32([[0, 1]], dev), i32([100], dev), i32([0, 3], dev), i32([5, 6, 7], dev))
+    assert torch.equal(sc.forward(q, *args, causal_granule=10 ** 15), sc.forward(q, *args, causal_granule=100))
+
+
 # ------------------------------------------------------------------------------------------------------ as one step
 class Server:
     """Requests that grow step by step through the four operators; the reference keeps plain lists."""
