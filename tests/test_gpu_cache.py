@@ -253,7 +253,7 @@ def make_store(rng, P, H, d, dev, fill=None):
         ora.values(*ora.quantise(v.numpy().astype(np.float64), ora.V_SCALES))
 
 
-def tolerance(dtype, q, k, out, spread, reach):
+def tolerance(dtype, q, k, v, out, spread, reach):
     """Bound of the error of one row of outputs.  With ds the error of a logit, a probability is off by 2 ds of itself at most
     (ds is small), and an output by that times sum p |v - out|: weights that all change alike leave it as it is.
 
@@ -261,8 +261,9 @@ def tolerance(dtype, q, k, out, spread, reach):
     what a term leaves is at most half its step of 1/4 for magnitudes up to 4, and the next term is taken of 16 times that: three
     terms (bf16) leave 2^-3 / 16^2, six (f32) 2^-3 / 16^5, and the factor two roundings.  Sums of d products in f32, 2^-24 a
     term, on sum |q k|; the accumulator starts at a number below |s| + 16, four roundings of that.  Probabilities are rounded to
-    f16, half a step of 2^-11, or in two terms 2^-22 (f32), and below 2^-21 of the largest to steps of 2^-31 of it; their sum is
-    taken before: an error on sum p |v|.  Sums of probabilities times values: f32, at most one rounding for 16 keys and 64
+    f16, half a step of 2^-11, or in two terms 2^-22 (f32), and their sum is taken before: an error on sum p |v|.  They are held as
+    2^7 p / p_max at least, and f16 has no steps below 2^-24: none is exact to more than 2^-32, half of that step, of the row's
+    sum, an error on sum |v|.  Sums of probabilities times values: f32, at most one rounding for 16 keys and 64
     more for shares and their join, on sum p |v|.  The result: one rounding of its type, and a quotient."""
     d, L = q.shape[0], k.shape[0]
     top = np.repeat(np.abs(q).reshape(-1, 32).max(1), 32)
@@ -270,7 +271,7 @@ def tolerance(dtype, q, k, out, spread, reach):
     s = np.abs(k) @ np.abs(q) / math.sqrt(d)
     ds = (np.abs(k) @ lost) / math.sqrt(d) + d * 2.0 ** -24 * s + 4 * 2.0 ** -24 * (s + 16)
     cut = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22
-    return (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * np.abs(out) + 2 * ds.max() * spread + cut * reach + L * 2.0 ** -31 * (spread + reach) \
+    return (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * np.abs(out) + 2 * ds.max() * spread + cut * reach + 2.0 ** -32 * np.abs(v).sum(0) \
         + (L / 16 + 64) * 2.0 ** -24 * reach
 
 
@@ -340,7 +341,7 @@ def check_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how="tokens", seed
             kk, vv = k[h // G][slots], v[h // G][slots]
             ref, spread, reach = ora.attend(qn[h, r0:r1], kk, vv, sees)
             for r in range(r1 - r0):
-                tol = tolerance(dtype, qn[h, r0 + r], kk if n else np.zeros((1, d)), ref[r], spread[r], reach[r])
+                tol = tolerance(dtype, qn[h, r0 + r], kk if n else np.zeros((1, d)), vv, ref[r], spread[r], reach[r])
                 err = np.abs(y[h, r0 + r] - ref[r])
                 assert (err <= tol).all(), (s, h, r, float((err / np.maximum(tol, 1e-300)).max()))
                 worst = max(worst, float((err / np.maximum(tol, 1e-300)).max()))
@@ -456,7 +457,7 @@ def test_forward_long_and_peaked(dev, dtype, peak):
     out = sc.forward(q, store, order[None].int(), i32([L], dev), i32([0, 1], dev), i32([L - 1], dev))
     kk, vv = (f64(x)[0, :L] for x in sc.read(store, slots, dtype=torch.float32))
     ref, spread, reach = ora.attend(f64(q)[0], kk, vv, np.ones((1, L), bool))
-    tol = tolerance(dtype, f64(q)[0, 0], kk, ref[0], spread[0], reach[0])
+    tol = tolerance(dtype, f64(q)[0, 0], kk, vv, ref[0], spread[0], reach[0])
     assert (np.abs(f64(out)[0, 0] - ref[0]) <= tol).all()
 
 
@@ -531,7 +532,7 @@ def test_forward_cut_into_pieces(dev, dtype, d, Hq, Hk, S, rows, lens, granule):
             top, sum_k = q[h, r0:r1].double().abs().amax(), kk.abs().sum(-1).amax()
             s_abs = top * sum_k / math.sqrt(d)
             ds = s_abs * ((2.0 ** -11 if dtype == "bf16" else 2.0 ** -23) / 3.75 + (d + 6) * 2.0 ** -24) + 64 * 2.0 ** -24
-            cut = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) + (length[s] / 16 + 64) * 2.0 ** -24 + length[s] * 2.0 ** -29
+            cut = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) + (length[s] / 16 + 64) * 2.0 ** -24 + length[s] * 2.0 ** -32
             bound = (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * ref.abs() + (4 * ds + cut) * vv.abs().amax()
             assert bool((err.abs() <= bound).all()), (s, h, float((err.abs() / bound).max()))
             off, norm = off + float(err.square().sum()), norm + float(ref.square().sum())
@@ -613,7 +614,7 @@ class Server:
                 kk, vv = ks[h // (self.Hq // self.Hk)], vs[h // (self.Hq // self.Hk)]
                 ref, spread, reach = ora.attend(f64(q[h, at:at + a]), kk, vv, sees)
                 for r in range(a):
-                    tol = tolerance(self.dtype, f64(q[h, at + r]), kk, ref[r], spread[r], reach[r])
+                    tol = tolerance(self.dtype, f64(q[h, at + r]), kk, vv, ref[r], spread[r], reach[r])
                     assert (np.abs(f64(out[h, at + r]) - ref[r]) <= tol).all(), (s, h, r)
             at += a
 
