@@ -37,13 +37,14 @@ typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kManyWaves = 4;                    // waves of a workgroup of cache_many_kernel, 32 query rows each
-constexpr int kFewTile = 16, kManyTile = 32 * kManyWaves;   // query rows of a piece
-constexpr int kFewRows = 48;                    // a request of more goes to cache_many_kernel
+constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
+// (token, head) rows of a request past which it goes to cache_many_kernel.  The two cross between 48 and 64 against 4,096 tokens
+// (8 requests: 24, 32, 48 and 64 rows 30, 30, 35 and 41 us on the few, 33, 33, 38 and 39 on the many), f32 at 48.
+constexpr int kFewRows = 48;
 constexpr int kFewSlots = 3072;                 // waves of cache_few_kernel that the GPU holds, 12 a compute unit
 constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (three at d = 64 are slower)
 constexpr int kRounds = 7;                      // fillings of those slots at most (below 8: a lane for each of eight requests)
-constexpr int kFewCost = 2, kManyCost = 8;      // what starting a piece and joining its result costs, in pages
+constexpr int kFewCost = 2, kManyCost = 12;     // what starting a piece and joining its result costs, in pages
 constexpr int kLeastPages = 2;                  // least pages of a piece
 constexpr int kRun = 16;                        // neighbouring pieces that a die gets in a row (an eighth of all: 17% slower on ragged requests)
 constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
@@ -368,13 +369,14 @@ __device__ __forceinline__ void store_run(void* out, long long at, f32x4 v, int 
     }
 }
 
-// f16 values of 2 N keys of each channel of a lane's bytes, BYTES bytes (two channels each) a key.  scale[k]: exponent of key k, as a
-// float of which the conversion reads the exponent only.  out[c]: channel c's keys, two a dword.
-template <int BYTES, int N>
-__device__ __forceinline__ void values_f16(const uint32_t* v, const float* scale, uint32_t (&out)[2 * BYTES][N]) {
+// Eight f16 values (keys) of each channel of a lane's bytes, BYTES bytes (two channels each) a key.  scale[k]: exponent of key k, as a
+// float of which the conversion reads the exponent only.
+template <int BYTES>
+__device__ __forceinline__ void values_f16(const uint32_t* v, const float (&scale)[8], f16x8* out) {
 #define SOL_CVT(w, s, sel) __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, sel))
+    u32x4 r[2 * BYTES];
 #pragma unroll
-    for (int j = 0; j < N; ++j) {   // keys 2j, 2j + 1
+    for (int j = 0; j < 4; ++j) {   // keys 2j, 2j + 1
 #pragma unroll
         for (int b = 0; b < BYTES; ++b) {
             uint32_t x, y;
@@ -385,10 +387,12 @@ __device__ __forceinline__ void values_f16(const uint32_t* v, const float* scale
                 x = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j], 2) : SOL_CVT(v[j >> 1], scale[2 * j], 0);
                 y = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j + 1], 3) : SOL_CVT(v[j >> 1], scale[2 * j + 1], 1);
             }
-            out[2 * b][j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-            out[2 * b + 1][j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            r[2 * b][j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            r[2 * b + 1][j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
     }
+#pragma unroll
+    for (int c = 0; c < 2 * BYTES; ++c) out[c] = __builtin_bit_cast(f16x8, r[c]);
 #undef SOL_CVT
 }
 
@@ -468,7 +472,9 @@ __device__ __forceinline__ float raise(float top, float& m, float& most, float& 
 // group g = l >> 4 holds channels 32g ... of the keys (16 x 16 x 128: one scale a lane; at d = 64 the upper groups hold
 // zeros).  Row 4g + e of key tile b of a 32-key window is key 8g + 4b + e: registers e of the tiles 0 and 1 are then the
 // eight consecutive keys that group g holds of the second product's operand.  Registers are filled again as soon as they
-// are used: the keys of the next page are on their way during the second product, its values during the next first one.
+// are used: the keys of the next page are on their way during the second product, its values during the next first one.  32-row
+// tiles need 256 registers and more (one wave a SIMD: 102 us against 65 at 48 requests of 200 to 32,000 tokens, 8 heads of 128
+// channels, 340 MB: 5.2 TB/s, a large copy reaches 4.9); this takes 165, three waves a SIMD.
 // ---------------------------------------------------------------------------
 template <int D>
 struct FewPage {
@@ -591,20 +597,14 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
             // 16 bytes: eight keys of two bytes (d = 128), or two runs of eight bytes (d = 64)
-            uint32_t w16[4][4];
             const uint32_t bytes[4] = {pg.v[w][c][0], pg.v[w][c][1], pg.v[w][c][2], pg.v[w][c][3]};
-            if constexpr (D == 128) {
-                values_f16<2, 4>(bytes, vs, w16);
-            } else {
-                uint32_t x[2][4], y[2][4];
-                values_f16<1, 4>(bytes, vs, x);
-                values_f16<1, 4>(bytes + 2, vs, y);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w16[0][i] = x[0][i], w16[1][i] = x[1][i], w16[2][i] = y[0][i], w16[3][i] = y[1][i];
-            }
             f16x8 va[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) va[t] = __builtin_bit_cast(f16x8, u32x4{w16[t][0], w16[t][1], w16[t][2], w16[t][3]});
+            if constexpr (D == 128) {
+                values_f16<2>(bytes, vs, va);
+            } else {
+                values_f16<1>(bytes, vs, va);
+                values_f16<1>(bytes + 2, vs, va + 2);
+            }
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 o[4 * c + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[t], ph, o[4 * c + t], 0, 0, 0);
@@ -711,6 +711,12 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
 // keys of D / 32 channels.  Two stages: while a page is used, the next one is converted from registers, and the one after is on its
 // way.  Row i of a 32-key window is key i with bits 2 and 3 exchanged, so that the registers 8u ... 8u + 7 of the first
 // product are the eight consecutive keys that a lane holds of the second one's operand.
+//
+// Bound by the power that the matrix products may draw: 3,600 rows of 40 heads over 75,600 tokens take 4.75 ms, 1,170 TFLOP/s, where
+// a large bf16 matrix product reaches 1,160 on the same card.  The bare instructions of a page, on random data from
+// registers, take 0.77 us a wave and page whether one, two or three waves share a SIMD, on constant data 0.55; here it is 0.85.
+// That leaves nothing for an order of the loop: products of the next page before the sums of this one, a window at a time
+// with three waves a SIMD, eight waves to a workgroup, values a step ahead of their use: all within 2% or slower.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ int swap23(int i) { return (i & 19) | ((i & 4) << 1) | ((i & 8) >> 1); }
 
@@ -721,30 +727,29 @@ struct Stage {
     uint32_t ks[64];                // scale bytes [chunk][window] of a lane
 };
 
-// A thread's part of a page: the first 256 threads (d = 64: 128) 16 bytes of keys, and thread t of 256 N the values of 8 / N keys of
-// the channel run i.
-template <int D, int N>
+// A thread's part of a page: 16 bytes of keys (d = 64: of the first 128 threads), and of the values eight keys of a channel run.
+template <int D>
 struct ManyPage {
-    u32x4 k;
-    uint32_t v[4 / N], vs[2 / N], ks;
+    u32x4 k, v;
+    u32x2 vs;
+    uint32_t ks;
 };
 
-template <int D, int N>
-__device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D, N>& r) {
+template <int D>
+__device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D>& r) {
     using L = PageLayout<D>;
     const unsigned t = threadIdx.x, lane = t & 63, i = lane & 31, h = lane >> 5;
     if (t < 2 * D) {
         const unsigned w = D == 128 ? t >> 7 : t >> 6, c = D == 128 ? (t >> 6) & 1 : 0;
         r.k = *reinterpret_cast<const u32x4*>(page + (L::k + (32 * w + swap23(i)) * (D / 2) + (2 * c + h) * 16));
     }
-    // d = 128: 16 / N bytes, d = 64: 8 / N
-    const uint32_t* v = reinterpret_cast<const uint32_t*>(page + (L::v + t * (D / (8 * N))));
-#pragma unroll
-    for (int x = 0; x < D / (32 * N); ++x) r.v[x] = v[x];
-    const unsigned oct = t / (32 * N), run = t / N % 32, part = t % N;
-    const uint32_t* vs = reinterpret_cast<const uint32_t*>(page + (L::vs + (oct * (D / 32) + run / (1024 / D)) * 8 + part * 4));
-#pragma unroll
-    for (int x = 0; x < 2 / N; ++x) r.vs[x] = vs[x];
+    if constexpr (D == 128) {
+        r.v = *reinterpret_cast<const u32x4*>(page + (L::v + t * 16));
+    } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(page + (L::v + t * 8));
+        r.v = u32x4{x[0], x[1], 0, 0};
+    }
+    r.vs = *reinterpret_cast<const u32x2*>(page + (L::vs + ((t >> 5) * (D / 32) + (t & 31) / (1024 / D)) * 8));
     if (t < 64) {
         if constexpr (D == 128) r.ks = *reinterpret_cast<const uint32_t*>(page + (L::ks + t * 4));
         else r.ks = *reinterpret_cast<const uint16_t*>(page + (L::ks + t * 2));
@@ -752,30 +757,26 @@ __device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D, N>& r
 }
 
 // left: tokens of the page that there are; what lies behind them may be anything, and a finite scale keeps 0 v = 0.
-template <int D, int N>
-__device__ __forceinline__ void many_store(const ManyPage<D, N>& r, Stage<D>& st, int left) {
+template <int D>
+__device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, int left) {
     constexpr int CT = D / 32;
-    const unsigned t = threadIdx.x;
+    const int t = threadIdx.x;
     if (t < 2 * D) st.k[t] = r.k;
     if (t < 64) st.ks[t] = r.ks;
-    const unsigned oct = t / (32 * N), run = t / N % 32, part = t % N;
-    float vs[8 / N];
-#pragma unroll
-    for (int x = 0; x < 2 / N; ++x) scales_of(r.vs[x], vs + 4 * x);
+    float vs[8];
+    scales_of(r.vs[0], vs);
+    scales_of(r.vs[1], vs + 4);
     if (left < kPage) {
-        asm volatile("" : "+s"(left));
+        asm volatile("" : "+s"(left));   // a branch, not instructions more for every page
 #pragma unroll
-        for (int i = 0; i < 8 / N; ++i)
-            if ((int)(8 * oct + 8 / N * part) + i >= left) vs[i] = 1.0f;
+        for (int i = 0; i < 8; ++i)
+            if (8 * (t >> 5) + i >= left) vs[i] = 1.0f;
     }
-    uint32_t va[CT][4 / N];
-    values_f16<D / 64, 4 / N>(r.v, vs, va);
+    const uint32_t bytes[4] = {r.v[0], r.v[1], r.v[2], r.v[3]};
+    f16x8 va[CT];
+    values_f16<D / 64>(bytes, vs, va);
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {   // keys 16 (oct / 2) + 8 (oct % 2) ...
-        uint32_t* to = reinterpret_cast<uint32_t*>(&st.v[((oct >> 1) * CT + c) * 64 + (oct & 1) * 32 + run]) + part * (4 / N);
-        if constexpr (N == 1) *reinterpret_cast<u32x4*>(to) = u32x4{va[c][0], va[c][1], va[c][2], va[c][3]};
-        else *reinterpret_cast<u32x2*>(to) = u32x2{va[c][0], va[c][1]};
-    }
+    for (int c = 0; c < CT; ++c) st.v[((t >> 6) * CT + c) * 64 + (t & 63)] = va[c];   // keys 16 (t >> 6) + 8 (t >> 5 & 1) ...
 }
 
 template <int D, bool F32T>
@@ -855,12 +856,12 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64 * kManyWaves, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
+__global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
                                                                                                        PartSpace* ws) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
     __shared__ Stage<D> stage[2];
-    __shared__ int s_last[kManyWaves];
+    __shared__ int s_last[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hk;
     Piece pc;
@@ -868,13 +869,12 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cache_many_kernel(const Ca
     const unsigned slot = pc.slot0 + (unsigned)pc.chunk * pc.tiles;
 
     // memory is asked for the first page, the rows' positions and the rows at once
-    constexpr int N = kManyWaves / 4;
     const long long page_stride = (long long)a.Hk * L::bytes;
     const uint8_t* store = a.store + (long long)pc.hk * L::bytes;
     Pages pages(a.table + (long long)pc.s * a.max_pages, a.P, pc.p0, pc.p1);
-    ManyPage<D, N> pg;
+    ManyPage<D> pg;
     int id = pages.next();
-    if (id >= 0) many_load<D, N>(store + id * page_stride, pg);
+    if (id >= 0) many_load<D>(store + id * page_stride, pg);
     const int r = pc.tile * kManyTile + 32 * wave + j;
     const bool valid = r < pc.rows;
     const int token = pc.row0 + (valid ? r / G : 0), head = pc.hk * G + (valid ? r % G : 0);
@@ -899,9 +899,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cache_many_kernel(const Ca
     least = __builtin_amdgcn_readfirstlane(least);
     if (lane == 0) s_last[wave] = last;
     __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < kManyWaves; ++w) all = max(all, s_last[w]);
+    const int all = max(max(s_last[0], s_last[1]), max(s_last[2], s_last[3]));
     bool more = pages.limit(__builtin_amdgcn_readfirstlane((all + kPage - 1) / kPage)) && id >= 0;
 
     f32x16 o[CT], off;
@@ -916,9 +914,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cache_many_kernel(const Ca
     // the page of tokens key0 ... is in stage[turn], the one after it in registers
     int turn = 0, key0 = pages.p * kPage;
     if (more) {
-        many_store<D, N>(pg, stage[0], pc.len - key0);
+        many_store<D>(pg, stage[0], pc.len - key0);
         id = pages.next();
-        if (id >= 0) many_load<D, N>(store + id * page_stride, pg);
+        if (id >= 0) many_load<D>(store + id * page_stride, pg);
     }
     __syncthreads();
     while (more) {
@@ -926,9 +924,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cache_many_kernel(const Ca
         more = id >= 0;
         if (more) {
             key0 = pages.p * kPage;
-            many_store<D, N>(pg, stage[turn ^ 1], pc.len - key0);
+            many_store<D>(pg, stage[turn ^ 1], pc.len - key0);
             id = pages.next();
-            if (id >= 0) many_load<D, N>(store + id * page_stride, pg);
+            if (id >= 0) many_load<D>(store + id * page_stride, pg);
         }
         if (now < last) many_page<D, F32T>(stage[turn], q, now, now + kPage > least, sees, m, most, off, l, o);
         turn ^= 1;
@@ -963,7 +961,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cache_many_kernel(const Ca
 // ---------------------------------------------------------------------------
 // Joins the shares of a tile's rows, of both kernels' pieces in one launch, in an order that the plan fixes.  D / 4 threads hold a row, four
 // channels each; where there are fewer rows than groups, the shares are dealt to several groups, whose sums are added in LDS.  Bound
-// by latency: the plan, the maxima, the sums.
+// by latency: the plan, the maxima, the sums: 5 to 7 us for single tokens; 60 us for 230 MB of a frame's shares.
 // ---------------------------------------------------------------------------
 constexpr int kJoinThreads = 512;
 
@@ -1104,7 +1102,7 @@ static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) 
     PartSpace* many_ws = p.many_bytes ? reinterpret_cast<PartSpace*>(static_cast<char*>(a.ws) + p.few_bytes) : nullptr;
     hipError_t e = hipSuccess;
     if (p.use_many) {
-        cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 64 * kManyWaves, 0, st>>>(a, p.many, scale_log2, many_ws);
+        cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 256, 0, st>>>(a, p.many, scale_log2, many_ws);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.use_few) {
