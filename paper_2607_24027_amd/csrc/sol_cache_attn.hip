@@ -712,7 +712,7 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
 // way.  Row i of a 32-key window is key i with bits 2 and 3 exchanged, so that the registers 8u ... 8u + 7 of the first
 // product are the eight consecutive keys that a lane holds of the second one's operand.
 //
-// Bound by the power that the matrix products may draw: 3,600 rows of 40 heads over 75,600 tokens take 4.75 ms, 1,170 TFLOP/s, where
+// Bound by what the matrix cores may draw: 3,600 rows of 40 heads over 75,600 tokens take 4.75 ms, 1,170 TFLOP/s, where
 // a large bf16 matrix product reaches 1,160 on the same card.  The bare instructions of a page, on random data from
 // registers, take 0.77 us a wave and page whether one, two or three waves share a SIMD, on constant data 0.55; here it is 0.85.
 // That leaves nothing for an order of the loop: products of the next page before the sums of this one, a window at a time
