@@ -89,7 +89,8 @@ int sol_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out,
  * ring: [P] i32, updated: the free pages, state[1] of them from ring[state[0]] on, around the
  *   end.  New pages come from its front, in the order of the requests; pages given back go
  *   to its end (a table entry that is not in [0, P) is not given back), so a page is
- *   used again as late as can be.
+ *   used again as late as can be.  A page that several requests share is given back once for each: the caller
+ *   takes it out of their tables (entry -1) before.
  * A request that would pass max_pages pages is refused; so is one for whose new pages the
  *   free ones do not suffice after those that the requests before it asked for.  A refused
  *   request keeps its length.

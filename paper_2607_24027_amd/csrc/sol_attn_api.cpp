@@ -172,7 +172,11 @@ int validate_forward(const void* q, const void* k, const void* v, const void* ou
 namespace sol {
 
 int set_error(int code, const char* text) {
-    g_err = text;
+    try {
+        g_err = text;
+    } catch (...) {   // no memory for the text: the code says enough
+        g_err.clear();
+    }
     return code;
 }
 

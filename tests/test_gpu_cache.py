@@ -542,6 +542,33 @@ def test_forward_cut_into_pieces(dev, dtype, d, Hq, Hk, S, rows, lens, granule):
     assert math.sqrt(off / norm) <= (2.0 ** -8 / math.sqrt(3) * 1.25 if dtype == "bf16" else 2.0 ** -20)
 
 
+def test_pages_past_four_gigabytes(dev):
+    """Pages whose bytes lie past 2^32 in the store, and pages that two requests share."""
+    P, H, d = 260000, 2, 128
+    assert P * H * 68 * d > 2 ** 32
+    store = torch.empty((P, H, 68 * d), dtype=torch.uint8, device=dev)
+    pages = [P - 1, 5, P - 2, 3, P // 2]
+    g = torch.Generator().manual_seed(9)
+    k, v = (torch.randn(H, 300, d, generator=g) for _ in range(2))
+    slots = np.array([pages[t // 64] * 64 + t % 64 for t in range(300)])
+    sc.append(k.to(dev), v.to(dev), store, i32(slots, dev))
+    kk, vv = (f64(x) for x in sc.read(store, i32(slots, dev), dtype=torch.float32))
+    assert np.array_equal(kk, ora.values(*ora.quantise(f64(k), ora.K_SCALES)))
+    assert np.array_equal(vv, ora.values(*ora.quantise(f64(v), ora.V_SCALES)))
+    rows = [1, 90]                       # the second request has the first three pages only, the first all
+    q = torch.randn(4, sum(rows), d, generator=g)
+    table = np.array([pages, pages[:3] + [-1, -1]])
+    out = f64(sc.forward(q.to(dev), store, i32(table, dev), i32([300, 190], dev), i32([0, 1, 91], dev),
+                         i32([299] + list(range(100, 190)), dev)))
+    for s, (r0, r1, n) in enumerate(((0, 1, 300), (1, 91, 190))):
+        pos = np.array([299]) if s == 0 else np.arange(100, 190)
+        for h in range(4):
+            ref, spread, reach = ora.attend(f64(q)[h, r0:r1], kk[h // 2, :n], vv[h // 2, :n], np.arange(n)[None] <= pos[:, None])
+            for r in range(r1 - r0):
+                tol = tolerance("f32", f64(q)[h, r0 + r], kk[h // 2, :n], vv[h // 2, :n], ref[r], spread[r], reach[r])
+                assert (np.abs(out[h, r0 + r] - ref[r]) <= tol).all()
+
+
 def test_empty_calls(dev):
     """No rows at all, and a granule past an int."""
     rng = np.random.default_rng(3)
