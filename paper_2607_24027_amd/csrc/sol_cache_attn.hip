@@ -41,10 +41,10 @@ constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
 // (token, head) rows of a request past which it goes to cache_many_kernel.  The two cross between 48 and 64 against 4,096 tokens
 // (8 requests: 24, 32, 48 and 64 rows 30, 30, 35 and 41 us on the few, 33, 33, 38 and 39 on the many), f32 at 48.
 constexpr int kFewRows = 48;
-constexpr int kFewSlots = 3072;                 // waves of cache_few_kernel that the GPU holds, 12 a compute unit
+constexpr int kFewSlots = 12 * 256;             // waves of cache_few_kernel that the GPU holds, 12 a compute unit
 constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (three at d = 64 are slower)
 constexpr int kRounds = 7;                      // fillings of those slots at most (below 8: a lane for each of eight requests)
-constexpr int kFewCost = 2, kManyCost = 12;     // what starting a piece and joining its result costs, in pages
+constexpr int kFewCost = 2, kManyCost = 20;     // what starting a piece and joining its result costs, in pages
 constexpr int kLeastPages = 2;                  // least pages of a piece
 constexpr int kRun = 16;                        // neighbouring pieces that a die gets in a row (an eighth of all: 17% slower on ragged requests)
 constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
@@ -125,7 +125,8 @@ __device__ __forceinline__ int pages_for(float pages, float tiles, int slots, in
 
 // Pages of a piece, at most: every tile of every request is cut into equal pieces of no more.  With few tiles, the pieces fill the slots
 // once; with many, it is chosen among fillings of one to kRounds times by the time that pieces dealt to free slots take, their
-// mean share and half a piece.  Past 64 requests (more loads for each lane) it is two fillings, or no cut at all.  By the
+// mean share and a quarter of a piece (half a piece and 12 pages a start: 2,048 rows over 6,144 tokens 300 us, 266 with these; 32
+// ragged requests 245, 260).  Past 64 requests (more loads for each lane) it is two fillings, or no cut at all.  By the
 // lanes of one wave, on values that all waves of a launch see alike.  `planned`: the choice as another launch made it (not read
 // where it is quicker formed again than fetched from memory that another die wrote).  r: the lane's request, of up to 64.
 __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& part, const int* planned, Request& r) {
@@ -147,7 +148,7 @@ __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& pa
         if (planned) return *planned;
         const float heads = (float)a.Hk;
         auto cost_of = [&](float pieces, float longest) {
-            return (sum + pieces * (float)part.cost) / (float)part.slots + 0.5f * (longest + (float)part.cost);
+            return (sum + pieces * (float)part.cost) / (float)part.slots + 0.25f * (longest + (float)part.cost);
         };
         float least = INFINITY;
         if (a.S <= 8) {   // lane 8 (k - 1) + s: all k at once (1.5 us less than one after the other)
