@@ -19,9 +19,9 @@
  * entries, positions) is never trusted with an address: each call states what it
  * does with values out of range.
  *
- * Sizes (B, N, T, S, heads, ...) are positive; a launch takes at most 2^27 tokens in
- * sol_qk_norm_rope, 2^28 tokens times heads in append and read, and in forward 2^24
- * tokens times query heads and 2^18 requests times key/value heads.
+ * Sizes (B, N, T, S, heads, ...) are positive; a launch takes at most 65,535 heads, 2^27
+ * tokens in sol_qk_norm_rope, 2^28 tokens times heads in append and read, and in forward
+ * 2^24 tokens times query heads and 2^18 requests times key/value heads.
  *
  * Strides are in elements; the d channels of a head are contiguous.  Rows that
  * are written must not overlap.  Tensors whose start and strides are multiples of

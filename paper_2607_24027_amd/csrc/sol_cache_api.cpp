@@ -35,7 +35,7 @@ int check_store(const void* store, int heads, int P) {
     if (!store) return fail(SOL_ERR_INVALID_ARG, "store must be non-null");
     if (reinterpret_cast<uintptr_t>(store) & 15) return fail(SOL_ERR_INVALID_ARG, "store must start on 16 bytes");
     if (heads <= 0 || P <= 0) return fail(SOL_ERR_INVALID_ARG, "heads and pages must be positive (got %d, %d)", heads, P);
-    if (P > (1 << 24)) return fail(SOL_ERR_UNSUPPORTED, "at most 16,777,216 pages (got %d)", P);
+    if (P > (1 << 24) || heads > 65535) return fail(SOL_ERR_UNSUPPORTED, "at most 16,777,216 pages of 65,535 heads (got %d, %d)", P, heads);
     return SOL_OK;
 }
 

@@ -130,6 +130,7 @@ __device__ __forceinline__ int pages_for(float pages, float tiles, int slots, in
 // lanes of one wave, on values that all waves of a launch see alike.  `planned`: the choice as another launch made it (not read
 // where it is quicker formed again than fetched from memory that another die wrote).  r: the lane's request, of up to 64.
 __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& part, const int* planned, Request& r) {
+#pragma clang fp contract(off)   // two kernels form the plan: the same roundings in both
     const int lane = threadIdx.x & 63, G = a.Hq / a.Hk;
     float sum = 0.f, tiles = 0.f;
     r = Request{};

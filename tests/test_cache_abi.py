@@ -93,6 +93,12 @@ def test_append_and_read_refusals(kw, code):
     assert sb.last_error()
 
 
+def test_too_many_heads():
+    for call in (append, read):
+        assert call(T=1, H=65536) == UNSUPPORTED
+        assert "65,535 heads" in sb.last_error()
+
+
 def attn(**kw):
     a = dict(q=A, sq=strides(1, 1), out=B_, so=strides(1, 1), store=C, table=D_, lens=E, row_start=F, positions=G, S=2, T=8, rows=4,
              Hq=8, Hk=2, d=128, P=100, MP=50, G=1, dtype=0, ws=H, ws_bytes=1 << 40)
