@@ -13,7 +13,7 @@
 //
 // Two kernels.  Requests of few rows: a wave takes 16 rows and a share of the keys, bytes of the cache go from memory to
 // registers (cache_few_kernel).  Others: four waves of 32 rows share tiles in LDS, whose values are converted
-// once for the 128 rows (cache_many_kernel).  Both cut the work of all requests into pieces of about the same number of pages,
+// once for the 128 rows (cache_many_kernel).  cache_mixed_kernel is both, for calls with requests of both.  Both cut the work of all requests into pieces of about the same number of pages,
 // whose partial results cache_join_kernel joins in the order of the keys.
 #include "sol_cache_internal.h"
 
@@ -617,8 +617,7 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
-                                                                                        PartSpace* ws) {
+__device__ __forceinline__ void few_piece(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned piece) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, CT = D / 16;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
@@ -626,8 +625,8 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
     Piece pc;
     Request request_of_lane;
     const int per = plan_pages(a, part, nullptr, request_of_lane);
-    if (blockIdx.x == 0 && ws && lane == 0) ws->per = per;
-    if (!find_piece<false>(a, part, per, request_of_lane, blockIdx.x, false, pc)) return;
+    if (piece == 0 && ws && lane == 0) ws->per = per;
+    if (!find_piece<false>(a, part, per, request_of_lane, piece, false, pc)) return;
 
     // memory is asked for the first page, the rows' positions and the rows at once
     const long long page_stride = (long long)a.Hk * L::bytes;
@@ -697,7 +696,7 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
                 store_run<F32T, VEC>(a.out, oi + CT * (4 * g + e) + t, f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]} * inv, 4);
         return;
     }
-    float* to = ws->results + (long long)blockIdx.x * (kFewTile * (D + 2));
+    float* to = ws->results + (long long)piece * (kFewTile * (D + 2));
     if (g == 0) to[2 * j] = most < 0.f ? kLowest : m, to[2 * j + 1] = l;
     float* po = to + 2 * kFewTile + j * D;
 #pragma unroll
@@ -705,6 +704,12 @@ __global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel
 #pragma unroll
         for (int t = 0; t < CT; t += 4)
             *reinterpret_cast<f32x4*>(po + CT * (4 * g + e) + t) = f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]};
+}
+
+template <int D, bool F32T, bool VEC>
+__global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
+                                                                                        PartSpace* ws) {
+    few_piece<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -858,8 +863,7 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
-                                                                                                       PartSpace* ws) {
+__device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned piece, unsigned pieces) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
     __shared__ Stage<D> stage[2];
@@ -867,7 +871,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hk;
     Piece pc;
-    if (!find_piece_shared<false>(a, part, ws, blockIdx.x, true, pc)) return;
+    if (!find_piece_shared<false>(a, part, ws, piece, true, pc)) return;
     const unsigned slot = pc.slot0 + (unsigned)pc.chunk * pc.tiles;
 
     // memory is asked for the first page, the rows' positions and the rows at once
@@ -949,7 +953,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
         }
         return;
     }
-    if (slot >= gridDim.x) return;   // rows that overlap: no room was asked for
+    if (slot >= pieces) return;   // rows that overlap: no room was asked for
     float* to = ws->results + (long long)slot * (kManyTile * (D + 2));
     const int row = 32 * wave + j;
     if (h == 0) to[2 * row] = most < 0.f ? kLowest : m, to[2 * row + 1] = l;
@@ -958,6 +962,25 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs 
     for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int t = 0; t < CT; ++t) po[CT * (8 * (i >> 2) + 4 * h + (i & 3)) + t] = o[t][i];
+}
+
+template <int D, bool F32T, bool VEC>
+__global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
+                                                                                                       PartSpace* ws) {
+    many_piece<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x, gridDim.x);
+}
+
+// Both in one launch: the many first (their pieces are the longest), then fours of the few, which fill what the last ones leave.
+template <int D, bool F32T, bool VEC>
+__global__ __launch_bounds__(256, 2) void cache_mixed_kernel(const CacheAttnArgs a, const Part few, const Part many, const float scale_log2,
+                                                             PartSpace* few_ws, PartSpace* many_ws, const unsigned few_pieces,
+                                                             const unsigned many_pieces) {
+    if (blockIdx.x < many_pieces) {
+        many_piece<D, F32T, VEC>(a, many, scale_log2, many_ws, blockIdx.x, many_pieces);
+    } else {
+        const unsigned piece = 4 * (blockIdx.x - many_pieces) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (piece < few_pieces) few_piece<D, F32T, VEC>(a, few, scale_log2, few_ws, piece);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1102,15 +1125,23 @@ static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) 
     const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)a.d));
     PartSpace* few_ws = p.few_bytes ? static_cast<PartSpace*>(a.ws) : nullptr;
     PartSpace* many_ws = p.many_bytes ? reinterpret_cast<PartSpace*>(static_cast<char*>(a.ws) + p.few_bytes) : nullptr;
-    hipError_t e = hipSuccess;
-    if (p.use_many) {
-        cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 256, 0, st>>>(a, p.many, scale_log2, many_ws);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+    // One launch for both kernels saves the second one's 4 to 8 us (8 requests of one token over 2,000, one of 256 rows: 52 and 45 us).
+    // Where that leaves the few two waves a SIMD instead of three (d = 128 in bf16, 64 in f32), it is slower once their keys take
+    // longer than a launch: 31 requests of one token and one of 512 rows, 8 heads of 128, 2,000, 4,000 and 16,000 tokens: 70, 78 and
+    // 162 us in two launches, 68, 77 and 171 in one.  The table bounds what there may be to read.
+    const bool one = p.use_many && p.use_few &&
+                     (F32T == (D == 128) || (long long)a.S * a.max_pages * a.Hk * PageLayout<D>::bytes <= 1 << 27);
+    if (one) {
+        const unsigned grid = (unsigned)(p.many_pieces + (p.few_pieces + 3) / 4);
+        cache_mixed_kernel<D, F32T, VEC><<<grid, 256, 0, st>>>(a, p.few, p.many, scale_log2, few_ws, many_ws, (unsigned)p.few_pieces,
+                                                               (unsigned)p.many_pieces);
+    } else {
+        if (p.use_many) cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 256, 0, st>>>(a, p.many, scale_log2, many_ws);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        if (p.use_few) cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_pieces, 64, 0, st>>>(a, p.few, scale_log2, few_ws);
     }
-    if (p.use_few) {
-        cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_pieces, 64, 0, st>>>(a, p.few, scale_log2, few_ws);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     JoinPart few{p.few, few_ws, (unsigned)p.few_pieces, few_ws ? (unsigned)p.few_tiles : 0u, (unsigned)p.few_quads, 4};
     // Few tiles have many shares each: a workgroup then takes fewer of a tile's rows, down to four (64 rows against 32,768
     // tokens of 8 heads: the call 47 us with 32 rows to a workgroup, 34 with four).

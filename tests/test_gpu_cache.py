@@ -276,7 +276,7 @@ def tolerance(dtype, q, k, v, out, spread, reach):
 
 
 def check_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how="tokens", seed=0, positions=None, drop=(), max_rows=None, extra=0,
-                  fill=255, atol_rows=None):
+                  fill=255, wide=0):
     """One call against the reference; lens: with the new rows."""
     rng = np.random.default_rng(seed)
     S = len(lens)
@@ -284,7 +284,7 @@ def check_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how="tokens", seed
     P = sum(held) + 2
     store, k, v = make_store(rng, P, Hk, d, dev)
     pages = rng.permutation(P)
-    MP = max(held + [1]) + 1
+    MP = max(held + [1]) + 1 + wide
     table = rng.integers(-1, 2 * P, (S, MP))                     # what lies behind a request's pages is never read
     at = 0
     raw = store.cpu().numpy()
@@ -371,6 +371,13 @@ FORWARD = [
 @pytest.mark.parametrize("d,Hq,Hk,lens,rows,granule,how", FORWARD)
 def test_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how):
     check_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how, seed=d + sum(lens))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("wide", [0, 4000])
+def test_forward_few_and_many_rows(dev, dtype, d, wide):
+    # requests of both kernels in one call; a table with room for long sequences gives each kernel its own launch
+    check_forward(dev, dtype, d, 8, 2, [700, 64, 333, 1500, 65, 200], [1, 2, 150, 90, 12, 1], 1, "tokens", seed=d, wide=wide)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
