@@ -292,10 +292,14 @@ __device__ __forceinline__ Split<NT> split_row(const float (&x)[32]) {
         const uint32_t byte = e + 127 - 4 * t;
         const float scale = __uint_as_float(byte << 23);
         r.w[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+        // The instruction writes its result before it has read all of its operands, which the compiler does not know: used behind it,
+        // they cannot share registers with the result (which made the last term wrong: errors of 3e-3 where 1.7e-3 is the rounding).
+        asm("" : "+v"(r.w[t]) : "v"(even), "v"(odd), "v"(scale));
         if (t % 4 == 0) r.scale[t / 4] = 0;
         r.scale[t / 4] |= byte << (8 * (t % 4));
         if (t + 1 < NT) {
-            const f32x32 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.w[t], scale);
+            f32x32 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.w[t], scale);
+            asm("" : "+v"(y) : "v"(r.w[t]), "v"(scale));   // likewise
 #pragma unroll
             for (int i = 0; i < 16; ++i) even[i] -= y[2 * i], odd[i] -= y[2 * i + 1];
         }

@@ -549,6 +549,44 @@ def test_forward_cut_into_pieces(dev, dtype, d, Hq, Hk, S, rows, lens, granule):
     assert math.sqrt(off / norm) <= (2.0 ** -8 / math.sqrt(3) * 1.25 if dtype == "bf16" else 2.0 ** -20)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("how", ["tokens", "odd"])
+@pytest.mark.parametrize("rows", [[3, 20, 1], [150], [3, 150, 1]])      # few rows, many, both in one call
+def test_forward_every_term_of_the_queries(dev, dtype, d, how, rows):
+    """The error over all values: a term of a query that is lost or wrong is 16 times what the terms leave.
+
+    Errors of independent values add up by their squares.  With keys and values that are independent and have the mean 0, a logit
+    that is off by e changes an output by e times what that key gives to it.  A channel of q, with the scaled top of its block in
+    (3.75, 7.5], is left with an error of at most 2^-11 top / 3.75 (bf16; f32: 2^-23), evenly spread: over sqrt(3).  d channels of keys
+    with squares k2 on average: sqrt(k2) times that, the 1 / sqrt(d) of the logits included.  Probabilities: half a step of 2^-11
+    over sqrt(3) (f32: 2^-22).  Results: half a step over sqrt(3); f32: 16 roundings of 2^-24 for sums."""
+    rng = np.random.default_rng(d + len(rows))
+    lens = [400, 350, 600][:len(rows)]
+    held = [-(-n // 64) for n in lens]
+    store, k, v = make_store(rng, sum(held), 2, d, dev)
+    pages = np.concatenate([[0], np.cumsum(held)])
+    table = np.full((len(rows), max(held) + 30), -1)
+    for s, n in enumerate(held):
+        table[s, :n] = np.arange(pages[s], pages[s] + n)
+    T = sum(rows)
+    q = torch.tensor(4.0 * rng.standard_normal((4, T, d)), dtype=torch.float32).to(DT[dtype])
+    row_start = np.concatenate([[0], np.cumsum(rows)])
+    positions = np.concatenate([np.full(r, n - 1) for n, r in zip(lens, rows)])
+    out = placed(torch.zeros(4, T, d, dtype=DT[dtype]), how, dev)
+    sc.forward(placed(q, how, dev), store, i32(table, dev), i32(lens, dev), i32(row_start, dev), i32(positions, dev), out=out)
+    y, qn = f64(out), f64(q)
+    off = norm = 0.0
+    for s, n in enumerate(lens):
+        at = slice(pages[s] * 64, pages[s] * 64 + n)
+        for h in range(4):
+            ref = ora.attend(qn[h, row_start[s]:row_start[s + 1]], k[h // 2, at], v[h // 2, at], np.ones((rows[s], n), bool))[0]
+            off, norm = off + np.square(y[h, row_start[s]:row_start[s + 1]] - ref).sum(), norm + np.square(ref).sum()
+    left = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -23) / 3.75 * np.abs(qn).max() * math.sqrt(np.square(k).mean())
+    parts = [left, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22, HALF_STEP[dtype] if dtype == "bf16" else 16 * 2.0 ** -24]
+    assert math.sqrt(off / norm) <= math.sqrt(sum(x * x for x in parts) / 3), math.sqrt(off / norm)
+
+
 def test_pages_past_four_gigabytes(dev):
     """Pages whose bytes lie past 2^32 in the store, and pages that two requests share."""
     P, H, d = 260000, 2, 128
