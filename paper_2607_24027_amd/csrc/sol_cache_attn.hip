@@ -12,7 +12,7 @@
 //   p . v   values are converted to f16 (exact), probabilities to f16 too: v_mfma_f32_*_f16.
 //
 // Two kernels.  Requests of few rows: a wave takes 16 rows and a share of the keys, bytes of the cache go from memory to
-// registers (cache_few_kernel).  Others: four waves of 32 rows share tiles in LDS, whose values are converted
+// registers (cache_few_kernel); short requests are not cut, or by the waves of a workgroup only.  Others: four waves of 32 rows share tiles in LDS, whose values are converted
 // once for the 128 rows (cache_many_kernel).  cache_mixed_kernel is both, for calls with requests of both.  Both cut the work of all requests into pieces of about the same number of pages,
 // whose partial results cache_join_kernel joins in the order of the keys.
 #include "sol_cache_internal.h"
@@ -41,13 +41,20 @@ constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
 // (token, head) rows of a request past which it goes to cache_many_kernel.  The two cross between 48 and 64 against 4,096 tokens
 // (8 requests: 24, 32, 48 and 64 rows 30, 30, 35 and 41 us on the few, 33, 33, 38 and 39 on the many), f32 at 48.
 constexpr int kFewRows = 48;
-constexpr int kFewSlots = 12 * 256;             // waves of cache_few_kernel that the GPU holds, 12 a compute unit
+constexpr int kFewWaves = 4;                    // waves of a workgroup of cache_few_kernel
+constexpr int kFewSlots = 12 * 256;             // waves of it that the GPU holds, 12 a compute unit
 constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (three at d = 64 are slower)
 constexpr int kRounds = 7;                      // fillings of those slots at most (below 8: a lane for each of eight requests)
 constexpr int kFewCost = 2, kManyCost = 20;     // what starting a piece and joining its result costs, in pages
 constexpr int kLeastPages = 2;                  // least pages of a piece
 constexpr int kRun = 16;                        // neighbouring pieces that a die gets in a row (an eighth of all: 17% slower on ragged requests)
+// Tiles of few rows from which each is a wave's, if the longest request has no more pages than that: a workgroup of four waves for each of
+// them is quicker for fewer (128 and 400 requests of 500 tokens, 8 heads: 20 and 66 us by workgroups, 19 and 49 by waves) and longer ones
+// (400 of 2,000: 178 and 210 us).
+constexpr int kManyTiles = 1024, kWavePages = 16;
 constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
+// "Pages of a piece" where no tile is cut: a tile is a wave's, or (few rows) a workgroup's.
+constexpr int kWave = 1 << 30, kWhole = INT_MAX;
 constexpr float kShift = 7.0f;   // probabilities are held as 2^7 p: f16 keeps all bits down to 2^-21 of the maximum's
 constexpr float kMost = 15.0f;   // exponent past which the running maximum is raised: 2^15 < 65504
 constexpr float kLowest = -3.402823466e38f;
@@ -68,6 +75,8 @@ struct Request {
 // Requests with rows in (LO, HI] take part.
 struct Part {
     int tile, slots, cost, lo, hi;
+    int whole;   // pages of the longest request up to which no tile is cut (0: the part of cache_many_kernel)
+    int uncut;   // kWave or kWhole where the table has no more, otherwise 0: a plan is formed
 };
 
 __device__ __forceinline__ Request request(const CacheAttnArgs& a, const Part& part, int s, int G) {
@@ -120,7 +129,7 @@ __device__ __forceinline__ float wave_max(float x) {
 // Pages of a piece, at most, by which `tiles` tiles of `pages` pages in all become no more pieces than fill the slots k times.
 __device__ __forceinline__ int pages_for(float pages, float tiles, int slots, int k) {
     const float room = (float)slots * (float)k - tiles;   // each tile rounds up by one piece at most
-    return room < 1.f ? 1 << 30 : (int)fmaxf(ceilf(pages / room), (float)kLeastPages);
+    return room < 1.f ? kWave : (int)fmaxf(ceilf(pages / room), (float)kLeastPages);
 }
 
 // Pages of a piece, at most: every tile of every request is cut into equal pieces of no more.  With few tiles, the pieces fill the slots
@@ -132,19 +141,33 @@ __device__ __forceinline__ int pages_for(float pages, float tiles, int slots, in
 __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& part, const int* planned, Request& r) {
 #pragma clang fp contract(off)   // two kernels form the plan: the same roundings in both
     const int lane = threadIdx.x & 63, G = a.Hq / a.Hk;
-    float sum = 0.f, tiles = 0.f;
+    float sum = 0.f, tiles = 0.f, longest = 0.f;
     r = Request{};
-    for (int s = lane; s < a.S; s += 64) {
+    if (part.uncut) {
+        if (lane < a.S) r = request(a, part, lane, G);   // past 64 they are read later
+        return part.uncut;
+    }
+    if (planned && a.S > 64) return *planned;
+    auto count = [&](int s) {
         r = request(a, part, s, G);
+        if (r.tiles) longest = fmaxf(longest, (float)r.pages);
         sum += (float)r.tiles * (float)r.pages;
         tiles += (float)r.tiles;
-    }
+    };
+    if (lane < a.S) count(lane);
+#pragma unroll 4
+    for (int s = lane + 64; s < a.S; s += 64) count(s);
     sum = at_lane(scan_add(sum), 63) * (float)a.Hk;
     tiles = at_lane(scan_add(tiles), 63) * (float)a.Hk;
+    longest = wave_max(longest);
+    // Few rows are not cut either where the longest request is at most twice what a workgroup has to read on average (300 requests of
+    // one token over 2,000, 8 heads: 168 us in pieces, 148 without; 31 over 8,000, at three times: 101 and 111).
+    if (part.whole && tiles >= kManyTiles && longest <= kWavePages) return kWave;
+    if (part.whole && longest <= fmaxf((float)part.whole, sum * (2.0f * kFewWaves / kFewSlots))) return kWhole;
     int per = pages_for(sum, tiles, part.slots, a.S > 64 ? 2 : 1);
     // Pieces of n pages make a join of pages / n shares, which it goes through in rounds of 16 of a row: the sum of n and the rounds
     // is least at the root (24 rows against 32,768 tokens of 8 heads: the call 34 us without this, 31 with it).
-    per = max(per, (int)ceilf(sqrtf(wave_max(r.tiles ? (float)r.pages : 0.f) * (1.0f / 16))));
+    per = max(per, (int)ceilf(sqrtf(longest * (1.0f / 16))));
     if (a.S <= 64 && tiles > 0.5f * (float)part.slots) {
         if (planned) return *planned;
         const float heads = (float)a.Hk;
@@ -254,7 +277,7 @@ __device__ __forceinline__ bool find_piece_shared(const CacheAttnArgs& a, const 
         Request r;
         const int per = plan_pages(a, part, JOIN ? &ws->per : nullptr, r);
         if (!JOIN && id == 0 && ws && threadIdx.x == 0) ws->per = per;
-        const bool found = find_piece<JOIN>(a, part, per, r, id, spread, out);
+        const bool found = !(JOIN && per >= kWave) && find_piece<JOIN>(a, part, per, r, id, spread, out);
         if (threadIdx.x == 0) s_piece = out, s_found = found;
     }
     __syncthreads();
@@ -620,17 +643,13 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
     }
 }
 
+// Row j of a wave's 16 against the piece's pages: running maximum (kLowest: it has seen no key), sum and sums of values of lane group 0 ... 3.
 template <int D, bool F32T, bool VEC>
-__device__ __forceinline__ void few_piece(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned piece) {
+__device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const Piece& pc, float scale_log2, float& m, float& l, f32x4 (&o)[D / 16]) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, CT = D / 16;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int G = a.Hq / a.Hk;
-    Piece pc;
-    Request request_of_lane;
-    const int per = plan_pages(a, part, nullptr, request_of_lane);
-    if (piece == 0 && ws && lane == 0) ws->per = per;
-    if (!find_piece<false>(a, part, per, request_of_lane, piece, false, pc)) return;
 
     // memory is asked for the first page, the rows' positions and the rows at once
     const long long page_stride = (long long)a.Hk * L::bytes;
@@ -665,10 +684,11 @@ __device__ __forceinline__ void few_piece(const CacheAttnArgs& a, const Part& pa
     least = __builtin_amdgcn_readfirstlane(least);
     if (!pages.limit((last + kPage - 1) / kPage)) id = -1;
 
-    f32x4 o[CT], s[4];
+    f32x4 s[4];
 #pragma unroll
     for (int t = 0; t < CT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = 0.f, most = -INFINITY, l = 0.f;
+    float most = -INFINITY;
+    m = l = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] *= scale_log2;
     const Split<NT> q = split_row<NT>(x);
@@ -688,32 +708,89 @@ __device__ __forceinline__ void few_piece(const CacheAttnArgs& a, const Part& pa
     while (id >= 0) step(std::true_type{});
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (!valid) return;
+    if (most < 0.f) m = kLowest;
+}
+
+// What the waves of a workgroup have found for one tile.
+template <int D>
+struct alignas(16) FewResults {
+    float o[kFewWaves][kFewTile][D + 4], ml[kFewWaves][kFewTile][2];
+};
+
+// A workgroup's part of the work: its waves share the pages of a tile where no tile is cut, and join their results in LDS; otherwise
+// each has a piece of its own.
+template <int D, bool F32T, bool VEC>
+__device__ __forceinline__ void few_block(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned block, unsigned pieces,
+                                          FewResults<D>& all) {
+    constexpr int CT = D / 16, LANES = D / 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, g = lane >> 4;
+    const int G = a.Hq / a.Hk;
+    Piece pc;
+    Request request_of_lane;
+    const int per = plan_pages(a, part, nullptr, request_of_lane);
+    if (block == 0 && ws && threadIdx.x == 0) ws->per = per;
+    const bool whole = per == kWhole;
+    const unsigned piece = whole ? block : kFewWaves * block + wave;
+    if (piece >= pieces || !find_piece<false>(a, part, per, request_of_lane, piece, false, pc)) return;
+    if (whole) {
+        const unsigned pages = pc.p1;
+        pc.p0 = (int)(pages * wave / kFewWaves), pc.p1 = (int)(pages * (wave + 1) / kFewWaves);
+    }
+    f32x4 o[CT];
+    float m, l;
+    few_rows<D, F32T, VEC>(a, pc, scale_log2, m, l, o);
     // register e of channel tile t is channel CT (4g + e) + t
-    if (pc.chunks == 1) {
+    const int r0 = pc.tile * kFewTile, rows = min(kFewTile, pc.rows - r0);
+    auto place = [&](int row) { return (pc.hk * G + (r0 + row) % G) * a.so.h + (pc.row0 + (r0 + row) / G) * a.so.n; };
+    if (whole) {
+        if (g == 0) all.ml[wave][j][0] = m, all.ml[wave][j][1] = l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t = 0; t < CT; t += 4)
+                *reinterpret_cast<f32x4*>(&all.o[wave][j][CT * (4 * g + e) + t]) = f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]};
+        __syncthreads();
+        const int at = 4 * (threadIdx.x % LANES);
+        for (int row = threadIdx.x / LANES; row < rows; row += 64 * kFewWaves / LANES) {
+            float top = kLowest;
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, all.ml[w][row][0]);
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) {
+                const float x = __builtin_amdgcn_exp2f(all.ml[w][row][0] - top);
+                l += x * all.ml[w][row][1];
+                sum += x * *reinterpret_cast<const f32x4*>(&all.o[w][row][at]);
+            }
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            store_run<F32T, VEC>(a.out, place(row) + at, sum * inv, 4);
+        }
+    } else if (j < rows && pc.chunks == 1) {
         const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const long long oi = head * a.so.h + token * a.so.n;
+        const long long oi = place(j);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int t = 0; t < CT; t += 4)
                 store_run<F32T, VEC>(a.out, oi + CT * (4 * g + e) + t, f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]} * inv, 4);
-        return;
+    } else if (j < rows) {
+        float* to = ws->results + (long long)piece * (kFewTile * (D + 2));
+        if (g == 0) to[2 * j] = m, to[2 * j + 1] = l;
+        float* po = to + 2 * kFewTile + j * D;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t = 0; t < CT; t += 4)
+                *reinterpret_cast<f32x4*>(po + CT * (4 * g + e) + t) = f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]};
     }
-    float* to = ws->results + (long long)piece * (kFewTile * (D + 2));
-    if (g == 0) to[2 * j] = most < 0.f ? kLowest : m, to[2 * j + 1] = l;
-    float* po = to + 2 * kFewTile + j * D;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int t = 0; t < CT; t += 4)
-            *reinterpret_cast<f32x4*>(po + CT * (4 * g + e) + t) = f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]};
 }
 
 template <int D, bool F32T, bool VEC>
-__global__ __launch_bounds__(64, F32T && D == 128 ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
-                                                                                        PartSpace* ws) {
-    few_piece<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x);
+__global__ __launch_bounds__(64 * kFewWaves, F32T && D == 128 ? 2 : 3) void cache_few_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
+                                                                                             PartSpace* ws, const unsigned pieces) {
+    __shared__ FewResults<D> results;
+    few_block<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x, pieces, results);
 }
 
 // ---------------------------------------------------------------------------
@@ -866,12 +943,19 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
     __builtin_amdgcn_s_setprio(0);
 }
 
+template <int D>
+struct ManySpace {
+    Stage<D> stage[2];
+    int last[4];
+};
+
 template <int D, bool F32T, bool VEC>
-__device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned piece, unsigned pieces) {
+__device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned piece, unsigned pieces,
+                                           ManySpace<D>& lds) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
-    __shared__ Stage<D> stage[2];
-    __shared__ int s_last[4];
+    Stage<D>* const stage = lds.stage;
+    int* const s_last = lds.last;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hk;
     Piece pc;
@@ -971,20 +1055,23 @@ __device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& p
 template <int D, bool F32T, bool VEC>
 __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
                                                                                                        PartSpace* ws) {
-    many_piece<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x, gridDim.x);
+    __shared__ ManySpace<D> lds;
+    many_piece<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x, gridDim.x, lds);
 }
 
-// Both in one launch: the many first (their pieces are the longest), then fours of the few, which fill what the last ones leave.
+// Both in one launch: the many first (their pieces are the longest), then the few, which fill what the last ones leave.
 template <int D, bool F32T, bool VEC>
 __global__ __launch_bounds__(256, 2) void cache_mixed_kernel(const CacheAttnArgs a, const Part few, const Part many, const float scale_log2,
                                                              PartSpace* few_ws, PartSpace* many_ws, const unsigned few_pieces,
                                                              const unsigned many_pieces) {
-    if (blockIdx.x < many_pieces) {
-        many_piece<D, F32T, VEC>(a, many, scale_log2, many_ws, blockIdx.x, many_pieces);
-    } else {
-        const unsigned piece = 4 * (blockIdx.x - many_pieces) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (piece < few_pieces) few_piece<D, F32T, VEC>(a, few, scale_log2, few_ws, piece);
-    }
+    static_assert(64 * kFewWaves == 256, "one shape of workgroups");
+    __shared__ union Space {
+        __device__ Space() {}
+        ManySpace<D> many;
+        FewResults<D> few;
+    } lds;
+    if (blockIdx.x < many_pieces) many_piece<D, F32T, VEC>(a, many, scale_log2, many_ws, blockIdx.x, many_pieces, lds.many);
+    else few_block<D, F32T, VEC>(a, few, scale_log2, few_ws, blockIdx.x - many_pieces, few_pieces, lds.few);
 }
 
 // ---------------------------------------------------------------------------
@@ -1079,6 +1166,7 @@ long long most_tiles(const Part& part, int S, int T, int max_rows, int Hq, int H
 // Pieces at most: what fills the slots kRounds times, or one for each tile; and no tile has more than its pages give.
 long long most_pieces(const Part& part, int S, int T, int max_rows, int Hq, int Hk, int max_pages) {
     const long long tiles = most_tiles(part, S, T, max_rows, Hq, Hk);
+    if (part.uncut) return tiles;
     // up to half the slots in tiles become one filling, more of them up to kRounds
     const long long rounds = tiles > part.slots / 2 || S > 64 ? kRounds : 1;
     return std::min(std::max(tiles, rounds * part.slots + kSlackPieces), tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
@@ -1087,7 +1175,7 @@ long long most_pieces(const Part& part, int S, int T, int max_rows, int Hq, int 
 struct Plan {
     Part few, many;
     bool use_few, use_many;
-    long long few_pieces, many_pieces, few_tiles, many_tiles;
+    long long few_pieces, many_pieces, few_tiles, many_tiles, few_blocks;
     size_t few_bytes, many_bytes;
     int few_quads;   // fours of rows of a tile of the few, at most
 };
@@ -1099,20 +1187,25 @@ Plan make_plan(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages)
     const long long most = (long long)std::min(max_rows, T) * (Hq / Hk);
     p.use_many = most > kFewRows;
     p.use_few = !p.use_many || S > 1;
-    p.few = {kFewTile, kFewSlots, kFewCost, 0, p.use_many ? kFewRows : INT_MAX};
-    p.many = {kManyTile, kManySlots, kManyCost, p.use_few ? kFewRows : 0, INT_MAX};
-    const bool join = max_pages > kLeastPages;   // otherwise a tile is one piece
+    p.few = {kFewTile, kFewSlots, kFewCost, 0, p.use_many ? kFewRows : INT_MAX, 0, 0};
+    p.many = {kManyTile, kManySlots, kManyCost, p.use_few ? kFewRows : 0, INT_MAX, 0, max_pages > kLeastPages ? 0 : kWave};
     if (p.use_few) {
         const int rows = p.use_many ? std::min(max_rows, std::max(1, kFewRows / (Hq / Hk))) : max_rows;
         p.few_quads = (int)(std::min<long long>((long long)rows * (Hq / Hk), kFewTile) + 3) / 4;
-        p.few_pieces = most_pieces(p.few, S, T, rows, Hq, Hk, max_pages);
         p.few_tiles = most_tiles(p.few, S, T, rows, Hq, Hk);
-        p.few_bytes = join ? kPartHeader + (size_t)p.few_pieces * kFewTile * (d + 2) * sizeof(float) : 0;
+        // Up to so many pages a tile is a workgroup's: no join, and no launch for it where the table has no more (8 requests of one token,
+        // 8 heads of 128: 1,000 tokens 12 us in pieces, 9 without, 2,000 tokens 13 and 14; 48 of them over 2,000: 29 and 23).  The
+        // tiles that there may be are up to half as many again as there are.
+        p.few.whole = p.few_tiles >= 128 ? 32 : 16;
+        if (max_pages <= p.few.whole) p.few.uncut = p.few_tiles >= kManyTiles / 2 * 3 && max_pages <= kWavePages ? kWave : kWhole;
+        p.few_pieces = most_pieces(p.few, S, T, rows, Hq, Hk, max_pages);
+        p.few_blocks = std::max(p.few_tiles, (p.few_pieces + kFewWaves - 1) / kFewWaves);
+        p.few_bytes = !p.few.uncut ? kPartHeader + (size_t)p.few_pieces * kFewTile * (d + 2) * sizeof(float) : 0;
     }
     if (p.use_many) {
         p.many_pieces = (most_pieces(p.many, S, T, max_rows, Hq, Hk, max_pages) / (8 * kRun) + 1) * 8 * kRun;   // whole turns of runs
         p.many_tiles = most_tiles(p.many, S, T, max_rows, Hq, Hk);
-        p.many_bytes = join ? kPartHeader + (size_t)p.many_pieces * kManyTile * (d + 2) * sizeof(float) : 0;
+        p.many_bytes = !p.many.uncut ? kPartHeader + (size_t)p.many_pieces * kManyTile * (d + 2) * sizeof(float) : 0;
     }
     return p;
 }
@@ -1136,13 +1229,13 @@ static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) 
     const bool one = p.use_many && p.use_few &&
                      (F32T == (D == 128) || (long long)a.S * a.max_pages * a.Hk * PageLayout<D>::bytes <= 1 << 27);
     if (one) {
-        const unsigned grid = (unsigned)(p.many_pieces + (p.few_pieces + 3) / 4);
+        const unsigned grid = (unsigned)(p.many_pieces + p.few_blocks);
         cache_mixed_kernel<D, F32T, VEC><<<grid, 256, 0, st>>>(a, p.few, p.many, scale_log2, few_ws, many_ws, (unsigned)p.few_pieces,
                                                                (unsigned)p.many_pieces);
     } else {
         if (p.use_many) cache_many_kernel<D, F32T, VEC><<<(unsigned)p.many_pieces, 256, 0, st>>>(a, p.many, scale_log2, many_ws);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        if (p.use_few) cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_pieces, 64, 0, st>>>(a, p.few, scale_log2, few_ws);
+        if (p.use_few) cache_few_kernel<D, F32T, VEC><<<(unsigned)p.few_blocks, 64 * kFewWaves, 0, st>>>(a, p.few, scale_log2, few_ws, (unsigned)p.few_pieces);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

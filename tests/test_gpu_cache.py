@@ -380,6 +380,17 @@ def test_forward_few_and_many_rows(dev, dtype, d, wide):
     check_forward(dev, dtype, d, 8, 2, [700, 64, 333, 1500, 65, 200], [1, 2, 150, 90, 12, 1], 1, "tokens", seed=d, wide=wide)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("S", [40, 200])
+@pytest.mark.parametrize("wide", [0, 100])
+def test_forward_short_requests(dev, dtype, d, S, wide):
+    # tiles that are not cut: a workgroup's (40 requests) or a wave's (200), by the table's width or by the lengths
+    rng = np.random.default_rng(S + d)
+    lens = [int(n) for n in rng.integers(0, 400, S)]
+    rows = [int(min(n, r)) for n, r in zip(lens, rng.integers(0, 3, S))]
+    check_forward(dev, dtype, d, 8, 8, lens, rows, 1, "tokens", seed=S, wide=wide, max_rows=2)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("fill", [0, 127, 254, 255])
 def test_forward_empty_requests_and_rows(dev, dtype, fill):
@@ -499,6 +510,8 @@ def test_forward_random(dev, seed):
     ("f32", 128, 16, 16, 12, 200, 900, 50),            # more than eight requests, one filling after the other
     ("bf16", 128, 4, 4, 90, 60, 500, 1),               # more requests than lanes, each of many rows
     ("f32", 64, 12, 12, 70, 3, 700, 1),                # more requests than lanes, each of few rows
+    ("bf16", 64, 8, 8, 90, 2, 3000, 1),                # few rows, lengths alike: not cut
+    ("bf16", 128, 4, 4, 30, 2, 4000, 1),               # few rows, cut
     ("bf16", 128, 8, 1, 1, 2, 200000, 1),              # one long request
 ])
 def test_forward_cut_into_pieces(dev, dtype, d, Hq, Hk, S, rows, lens, granule):
