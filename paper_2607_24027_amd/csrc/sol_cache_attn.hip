@@ -41,6 +41,10 @@ constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
 // (token, head) rows of a request past which it goes to cache_many_kernel.  The two cross between 48 and 64 against 4,096 tokens
 // (8 requests: 24, 32, 48 and 64 rows 30, 30, 35 and 41 us on the few, 33, 33, 38 and 39 on the many), f32 at 48.
 constexpr int kFewRows = 48;
+// With a table of no more pages and no more rows than that in all, every request is one of few rows: a workgroup for 16 rows fills the
+// GPU sooner (one and 8 requests of 64 tokens over 1,000, 32 heads: 22 and 38 us on the many, 10 and 25 on the few; 48 of them 73 and 88).
+constexpr int kShortPages = 32, kShortRows = 16 * 1024;
+constexpr int kManyWhole = 8;                   // pages of a table up to which many rows are not cut
 constexpr int kFewWaves = 4;                    // waves of a workgroup of cache_few_kernel
 constexpr int kFewSlots = 12 * 256;             // waves of it that the GPU holds, 12 a compute unit
 constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (three at d = 64 are slower)
@@ -75,8 +79,9 @@ struct Request {
 // Requests with rows in (LO, HI] take part.
 struct Part {
     int tile, slots, cost, lo, hi;
-    int whole;   // pages of the longest request up to which no tile is cut (0: the part of cache_many_kernel)
+    int whole;   // few rows: pages of the longest request up to which no tile is cut
     int uncut;   // kWave or kWhole where the table has no more, otherwise 0: a plan is formed
+    bool few;    // the part of cache_few_kernel
 };
 
 __device__ __forceinline__ Request request(const CacheAttnArgs& a, const Part& part, int s, int G) {
@@ -162,8 +167,11 @@ __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& pa
     longest = wave_max(longest);
     // Few rows are not cut either where the longest request is at most twice what a workgroup has to read on average (300 requests of
     // one token over 2,000, 8 heads: 168 us in pieces, 148 without; 31 over 8,000, at three times: 101 and 111).
-    if (part.whole && tiles >= kManyTiles && longest <= kWavePages) return kWave;
-    if (part.whole && longest <= fmaxf((float)part.whole, sum * (2.0f * kFewWaves / kFewSlots))) return kWhole;
+    // Many rows: not cut for requests of up to a page for four tiles (8 and 48 requests of 16 tokens over 1,000, 8 heads: 27 and 56 us
+    // in pieces, 25 and 39 without; 48 over 3,000: 96 and 89).
+    if (!part.few && longest <= fminf(0.25f * tiles, 64.f)) return kWave;
+    if (part.few && tiles >= kManyTiles && longest <= kWavePages) return kWave;
+    if (part.few && longest <= fmaxf((float)part.whole, sum * (2.0f * kFewWaves / kFewSlots))) return kWhole;
     int per = pages_for(sum, tiles, part.slots, a.S > 64 ? 2 : 1);
     // Pieces of n pages make a join of pages / n shares, which it goes through in rounds of 16 of a row: the sum of n and the rounds
     // is least at the root (24 rows against 32,768 tokens of 8 heads: the call 34 us without this, 31 with it).
@@ -1186,10 +1194,10 @@ struct Plan {
 Plan make_plan(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages) {
     Plan p{};
     const long long most = (long long)std::min(max_rows, T) * (Hq / Hk);
-    p.use_many = most > kFewRows;
+    p.use_many = most > kFewRows && (max_pages > kShortPages || (long long)T * Hq > kShortRows);
     p.use_few = !p.use_many || S > 1;
-    p.few = {kFewTile, kFewSlots, kFewCost, 0, p.use_many ? kFewRows : INT_MAX, 0, 0};
-    p.many = {kManyTile, kManySlots, kManyCost, p.use_few ? kFewRows : 0, INT_MAX, 0, max_pages > kLeastPages ? 0 : kWave};
+    p.few = {kFewTile, kFewSlots, kFewCost, 0, p.use_many ? kFewRows : INT_MAX, 0, 0, true};
+    p.many = {kManyTile, kManySlots, kManyCost, p.use_few ? kFewRows : 0, INT_MAX, 0, max_pages > kManyWhole ? 0 : kWave, false};
     if (p.use_few) {
         const int rows = p.use_many ? std::min(max_rows, std::max(1, kFewRows / (Hq / Hk))) : max_rows;
         p.few_quads = (int)(std::min<long long>((long long)rows * (Hq / Hk), kFewTile) + 3) / 4;

@@ -380,6 +380,14 @@ def test_forward_few_and_many_rows(dev, dtype, d, wide):
     check_forward(dev, dtype, d, 8, 2, [700, 64, 333, 1500, 65, 200], [1, 2, 150, 90, 12, 1], 1, "tokens", seed=d, wide=wide)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("wide", [0, 6, 60])
+def test_forward_short_prefills(dev, dtype, wide):
+    # many rows, not cut: by few rows' kernel, by the table's width, by the tiles; 2,049 rows of 8 heads are too many for the first
+    rows = [256, 255, 256, 1, 256, 256, 256, 256, 257] if wide == 6 else [100, 300, 1, 200]
+    check_forward(dev, dtype, 64, 8 if wide == 6 else 4, 2, [n + 20 for n in rows], rows, 1, "tokens", seed=wide, wide=wide)
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
 @pytest.mark.parametrize("S", [40, 200])
 @pytest.mark.parametrize("wide", [0, 100])
@@ -411,12 +419,13 @@ def test_forward_max_rows_leaves_the_rest(dev, rows):
     rng = np.random.default_rng(5)
     store, _, _ = make_store(rng, 8, 1, 128, dev)
     q = torch.randn(2, sum(rows), 128, device=dev)
-    args = (store, i32([[0, 1, 2, 3], [4, 5, 6, 7]], dev), i32([250, 256], dev), i32(np.cumsum([0] + rows), dev),
+    table = np.pad([[0, 1, 2, 3], [4, 5, 6, 7]], ((0, 0), (0, 60)), constant_values=-1)      # wide enough to need a workspace
+    args = (store, i32(table, dev), i32([250, 256], dev), i32(np.cumsum([0] + rows), dev),
             i32(list(range(rows[0])) + list(range(rows[1])), dev))
     full = sc.forward(q, *args)
     part = sc.forward(q, *args, max_rows=max(rows))
     assert torch.equal(full, part)
-    workspace = torch.empty(sc.workspace_bytes(2, sum(rows), max(rows), 2, 1, 128, 4), dtype=torch.uint8, device=dev)
+    workspace = torch.empty(sc.workspace_bytes(2, sum(rows), max(rows), 2, 1, 128, 64), dtype=torch.uint8, device=dev)
     assert torch.equal(sc.forward(q, *args, max_rows=max(rows), workspace=workspace), full)
     with pytest.raises(sb.SolAttnError):
         sc.forward(q, *args, max_rows=max(rows), workspace=workspace[:16])
