@@ -510,8 +510,8 @@ __device__ __forceinline__ float raise(float top, float& m, float& most, float& 
 // zeros).  Row 4g + e of key tile b of a 32-key window is key 8g + 4b + e: registers e of the tiles 0 and 1 are then the
 // eight consecutive keys that group g holds of the second product's operand.  Registers are filled again as soon as they
 // are used: the keys of the next page are on their way during the second product, its values during the next first one.  32-row
-// tiles need 256 registers and more (one wave a SIMD: 102 us against 65 at 48 requests of 200 to 32,000 tokens, 8 heads of 128
-// channels, 340 MB: 5.2 TB/s, a large copy reaches 4.9); this takes 165, three waves a SIMD.
+// tiles need 256 registers and more (one wave a SIMD: 102 us against 66 at 48 requests of 200 to 32,000 tokens, 8 heads of 128
+// channels, 340 MB: 5.1 TB/s, a large copy reaches 4.9); this takes 165, three waves a SIMD.
 // ---------------------------------------------------------------------------
 template <int D>
 struct FewPage {
@@ -808,8 +808,8 @@ __global__ __launch_bounds__(64 * kFewWaves, F32T && D == 128 ? 2 : 3) void cach
 // way.  Row i of a 32-key window is key i with bits 2 and 3 exchanged, so that the registers 8u ... 8u + 7 of the first
 // product are the eight consecutive keys that a lane holds of the second one's operand.
 //
-// Bound by what the matrix cores may draw: 3,600 rows of 40 heads over 75,600 tokens take 4.75 ms, 1,170 TFLOP/s, where
-// a large bf16 matrix product reaches 1,160 on the same card.  The bare instructions of a page, on random data from
+// Bound by what the matrix cores may draw: 3,600 rows of 40 heads over 75,600 tokens take 4.75 to 5.0 ms by the card, 1,110 to
+// 1,170 TFLOP/s at 1.9 GHz, where a large bf16 matrix product reaches 1,160.  The bare instructions of a page, on random data from
 // registers, take 0.77 us a wave and page whether one, two or three waves share a SIMD, on constant data 0.55; here it is 0.85.
 // That leaves nothing for an order of the loop: products of the next page before the sums of this one, a window at a time
 // with three waves a SIMD, eight waves to a workgroup, values a step ahead of their use: all within 2% or slower.
