@@ -56,6 +56,7 @@ constexpr int kRun = 16;                        // neighbouring pieces that a di
 // them is quicker for fewer (128 and 400 requests of 500 tokens, 8 heads: 20 and 66 us by workgroups, 19 and 49 by waves) and longer ones
 // (400 of 2,000: 178 and 210 us).
 constexpr int kManyTiles = 1024, kWavePages = 16;
+constexpr float kFewJoin = 1.f / 512, kManyJoin = 1.f / 32;   // what writing and reading a piece's result takes, in pages of a piece
 constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
 // "Pages of a piece" where no tile is cut: a tile is a wave's, or (few rows) a workgroup's.
 constexpr int kWave = 1 << 30, kWhole = INT_MAX;
@@ -174,8 +175,10 @@ __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& pa
     if (part.few && longest <= fmaxf((float)part.whole, sum * (2.0f * kFewWaves / kFewSlots))) return kWhole;
     int per = pages_for(sum, tiles, part.slots, a.S > 64 ? 2 : 1);
     // Pieces of n pages make a join of pages / n shares, which it goes through in rounds of 16 of a row: the sum of n and the rounds
-    // is least at the root (24 rows against 32,768 tokens of 8 heads: the call 34 us without this, 31 with it).
-    per = max(per, (int)ceilf(sqrtf(longest * (1.0f / 16))));
+    // is least at the root (24 rows against 32,768 tokens of 8 heads: the call 34 us without this, 31 with it).  So is the sum of n and
+    // the results of all pages / n pieces, 66 kB each of 128 rows (64 and 128 rows of 32 heads over 2,500 tokens: 31 and 35 us
+    // without, 25 and 30 with it; f32, 48 requests of one row of 16 heads over 3,000: 33 and 27).
+    per = max(per, (int)ceilf(sqrtf(fmaxf(longest * (1.0f / 16), sum * (part.few ? kFewJoin : kManyJoin)))));
     if (a.S <= 64 && tiles > 0.5f * (float)part.slots) {
         if (planned) return *planned;
         const float heads = (float)a.Hk;
