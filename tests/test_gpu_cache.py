@@ -513,6 +513,82 @@ def test_forward_random(dev, seed):
                   seed=seed, positions=positions, drop=drop, extra=0)
 
 
+# The same edges where requests are cut into pieces and rows go to both kernels: tables with room for long sequences.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,Hq,Hk,lens,rows,granule,how", FORWARD)
+def test_forward_wide_tables(dev, dtype, d, Hq, Hk, lens, rows, granule, how):
+    check_forward(dev, dtype, d, Hq, Hk, lens, rows, granule, how, seed=d + sum(lens), wide=40)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fill", [0, 127, 254, 255])
+@pytest.mark.parametrize("rows", [3, 70])
+def test_forward_cut_rows_that_see_nothing(dev, dtype, fill, rows):
+    positions = np.concatenate([np.resize([-1, 0, 2100, 89, -1, 2199], rows), [2, 3, 3]])
+    check_forward(dev, dtype, 64, 4, 2, [2200, 0, 70, 0, 4], [rows, 0, 2, 0, 1], 1, positions=positions, fill=fill, seed=fill, wide=40)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 150])
+def test_forward_cut_dropped_pages(dev, dtype, rows):
+    drop = [(0, p, -1) for p in (0, 3, 4, 5, 6, 7, 8, 30)] + [(0, 20, 1 << 30), (0, 39, -(1 << 31))] + [(1, p, -1) for p in range(40)]
+    check_forward(dev, dtype, 128, 4, 2, [2560, 2500], [rows, rows], 1, drop=drop, seed=rows, wide=40)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [3, 130])
+def test_forward_cut_not_finite(dev, dtype, d, T):
+    # as test_forward_not_finite, of pieces that are joined
+    rng = np.random.default_rng(T)
+    L = 3000
+    P = -(-L // 64)
+    k, v = (torch.tensor(rng.standard_normal((1, P * 64, d)), dtype=torch.float32, device=dev) for _ in range(2))
+    q = torch.tensor(rng.standard_normal((2, T, d)), dtype=torch.float32, device=dev).to(DT[dtype])
+    order = torch.tensor(rng.permutation(P), device=dev)
+    slots = (order[:, None] * 64 + torch.arange(64, device=dev)).flatten().int()
+    table = torch.nn.functional.pad(order[None].int(), (0, 40), value=-1)
+    positions = i32(np.linspace(L - 1, 700, T), dev)
+
+    def run(bad_k=None, bad_v=None, bad_q=None):
+        kk, vv, qq = k.clone(), v.clone(), q.clone()
+        if bad_k is not None:
+            kk[0, bad_k, 7] = math.nan
+        if bad_v is not None:
+            vv[0, bad_v, 3] = -math.inf
+        if bad_q is not None:
+            qq[1, bad_q, 10] = math.nan
+        store = sc.empty(P, 1, d, dev)
+        sc.append(kk, vv, store, slots)
+        return sc.forward(qq, store, table, i32([L], dev), i32([0, T], dev), positions)
+    clean = run()
+    assert bool(torch.isfinite(clean).all())
+    for kw in (dict(bad_k=0), dict(bad_k=1500), dict(bad_v=2900), dict(bad_k=2999)):
+        at = next(iter(kw.values()))
+        y = run(**kw)
+        sees = (positions >= at)[None, :, None].expand_as(y)
+        assert bool(torch.isnan(y[sees]).all()) and torch.equal(y[~sees], clean[~sees])
+    y = run(bad_q=1)
+    assert bool(torch.isnan(y[1, 1]).all())
+    y[1, 1] = clean[1, 1]
+    assert torch.equal(y, clean)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_forward_random_wide(dev, seed):
+    rng = np.random.default_rng(3000 + seed)
+    d = int(rng.choice([64, 128]))
+    Hk, G = int(rng.integers(1, 4)), int(rng.choice([1, 2, 4, 7]))
+    S = int(rng.integers(1, 12))
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(2500), S))]
+    rows = [int(rng.integers(0, max(2, min(n, 2000 // (S * Hk * G))) + 1)) for n in lens]
+    rows[0] = max(1, rows[0])
+    positions = np.concatenate([rng.integers(-1, n + 3, r) for n, r in zip(lens, rows)])
+    drop = [(s, int(rng.integers(0, -(-n // 64))), int(rng.choice([-1, 1 << 28]))) for s, n in enumerate(lens) if rng.random() < 0.3 and n]
+    check_forward(dev, str(rng.choice(["bf16", "f32"])), d, Hk * G, Hk, lens, rows, int(rng.choice([1, 17, 300, 1 << 30])),
+                  str(rng.choice(["plain", "tokens", "odd"])), seed=seed, positions=positions, drop=drop, wide=int(rng.choice([40, 5000])))
+
+
 @pytest.mark.parametrize("dtype,d,Hq,Hk,S,rows,lens,granule", [
     ("bf16", 128, 32, 16, 1, 700, 5000, 1),            # one request, tiles of 128 rows past half of what the GPU holds, cut
     ("bf16", 64, 64, 16, 3, 300, 2500, 1 << 30),       # few requests, all fillings looked at at once
