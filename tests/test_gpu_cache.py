@@ -883,3 +883,89 @@ def test_streams_of_their_own(dev):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(x, want[i]) for x in got[i])
+
+
+# ------------------------------------------------------------------------------------------------ the plan of pieces
+FEW_TILE, MANY_TILE, HEADER, SENTINEL = 16, 128, 256, 0x5A5A5A5A
+
+
+def pages_of_pieces(ws, d, need, both):
+    """Pages of a piece as the parts of a call planned them: the words in front of the parts' results.  A workspace that held the
+    sentinel before has that word, 63 untouched ones and the results; the second part starts behind a whole number of results of
+    16 rows of the first and ends with a whole number of 128 results of 128 rows."""
+    w = ws.view(torch.int32).cpu().numpy()
+
+    def header(at):
+        return w[at // 4] != SENTINEL and (w[at // 4 + 1:at // 4 + HEADER // 4] == SENTINEL).all()
+    assert header(0)
+    if not both:
+        return [int(w[0])]
+    few, many = FEW_TILE * (d + 2) * 4, 128 * MANY_TILE * (d + 2) * 4
+    at = [a for a in range(HEADER, need - many, few) if (need - a - HEADER) % many == 0 and header(a)]
+    assert len(at) == 1, at
+    return [int(w[0]), int(w[at[0] // 4])]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("Hq,Hk,S,rows,lens,parts", [
+    # parts: for the few and the many rows, least and most pages of a piece; None: the part is not there
+    (32, 8, 4, [300], [4500, 1800], [None, (2, 60)]),             # few requests, all fillings at once
+    (16, 8, 12, [200], [5000, 900], [None, (2, 60)]),             # one filling after the other
+    (4, 4, 70, [60], [6000, 300], [None, (2, 60)]),               # more requests than lanes
+    (4, 4, 150, [60, 1, 2], [6000, 300], [(2, 60), (2, 60)]),     # the same, of both kinds (rows of the long ones: 60 and 1)
+    (3, 3, 90, [2, 1], [5000, 200], [(2, 60), None]),             # the same, of few rows
+    (70, 70, 8, [40], [3000, 400], [(2, 40), None]),              # few rows: all fillings at once
+    (34, 34, 60, [1], [4000, 300], [(2, 50), None]),              # few rows: one filling after the other
+])
+def test_forward_every_way_of_cutting(dev, dtype, d, Hq, Hk, S, rows, lens, parts):
+    """Every way in which the pages of a piece are chosen, each shown by what the plan left in the workspace: less than the longest
+    request has.  One request of each part in the middle is long (lens[0] tokens), the others have half of lens[1] to lens[1]."""
+    rng = np.random.default_rng(S)
+    length = [int(lens[1] * f) for f in rng.uniform(0.5, 1.0, S)]
+    few_too = parts[1] is not None and parts[0] is not None
+    length[S // 2:S // 2 + 1 + few_too] = [lens[0]] * (1 + few_too)
+    rows = [rows[s % len(rows)] for s in range(S)]
+    held = [-(-n // 64) for n in length]
+    start, P, T = np.cumsum([0] + held), sum(held), sum(rows)
+    g = torch.Generator(device=dev).manual_seed(S)
+    k, v = (torch.randn(Hk, P * 64, d, generator=g, device=dev) for _ in range(2))
+    store = sc.empty(P, Hk, d, dev)
+    order = torch.randperm(P, generator=g, device=dev)
+    slots = (order[:, None] * 64 + torch.arange(64, device=dev)).flatten().int()
+    sc.append(k, v, store, slots)
+    k, v = (x.double() for x in sc.read(store, slots, dtype=torch.float32))
+    table = torch.full((S, max(held) + 3), -1, dtype=torch.int32, device=dev)
+    for s in range(S):
+        table[s, :held[s]] = order[start[s]:start[s + 1]].int()
+    q = torch.randn(T, Hq, d, generator=g, device=dev).to(DT[dtype]).transpose(0, 1)
+    row_start = np.cumsum([0] + rows)
+    positions = torch.cat([torch.arange(n - r, n, dtype=torch.int32, device=dev) for n, r in zip(length, rows)])
+    need = sc.workspace_bytes(S, T, max(rows), Hq, Hk, d, table.shape[1])
+    ws = torch.full((need,), 0x5A, dtype=torch.uint8, device=dev)
+    out = sc.forward(q, store, table, i32(length, dev), i32(row_start, dev), positions, max_rows=max(rows), workspace=ws)
+    # with the many rows' kernel and several requests, the few rows' part is there too, even if no request is for it
+    per = pages_of_pieces(ws, d, need, both=parts[1] is not None)
+    for part, got in zip(parts, per):
+        if part is not None:
+            assert part[0] <= got <= part[1], per
+    off = norm = 0.0
+    for s in range(S):
+        r0, r1, k0 = row_start[s], row_start[s + 1], start[s] * 64
+        hidden = torch.arange(length[s], device=dev)[None] > positions[r0:r1, None]
+        for h in range(Hk):
+            kk, vv = (x[h, k0:k0 + length[s]] for x in (k, v))
+            qq = q[h * (Hq // Hk):(h + 1) * (Hq // Hk), r0:r1].double()
+            logits = (qq.reshape(-1, d) @ kk.T.contiguous()).view(Hq // Hk, r1 - r0, -1) / math.sqrt(d)
+            p = torch.softmax(logits.masked_fill(hidden, -math.inf), -1).flatten(0, 1)
+            ref, reach = p @ vv, p @ vv.abs()
+            err = out[h * (Hq // Hk):(h + 1) * (Hq // Hk), r0:r1].double().reshape(-1, d) - ref
+            # as in tolerance(), with the largest |q| for that of a block, and 2 sum p |v| for sum p |v - out|; a third term of the
+            # queries leaves half a step of 2^-3 (its values reach 2), so three leave 2^-4 / 16^2, six 2^-4 / 16^5
+            s_abs = qq.abs().amax() * kk.abs().sum(-1).amax() / math.sqrt(d)
+            ds = s_abs * ((2.0 ** -12 if dtype == "bf16" else 2.0 ** -24) / 3.75 + (d + 6) * 2.0 ** -24) + 64 * 2.0 ** -24
+            cut = (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) + (length[s] / 16 + 64) * 2.0 ** -24
+            bound = (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * ref.abs() + (4 * ds + cut) * reach + 2.0 ** -32 * vv.abs().sum(0)
+            assert bool((err.abs() <= bound).all()), (s, h, float((err.abs() / bound).max()))
+            off, norm = off + float(err.square().sum()), norm + float(ref.square().sum())
+    # over all values: as in test_forward_cut_into_pieces
+    assert math.sqrt(off / norm) <= (2.0 ** -8 / math.sqrt(3) * 1.25 if dtype == "bf16" else 2.0 ** -20)
