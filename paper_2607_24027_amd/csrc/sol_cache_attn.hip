@@ -9,7 +9,8 @@
 //           ones (32 against 64 cycles for 32 x 32 x 64), and sums of their products lose nothing, where those of 8-bit
 //           floats, whose exponents reach further, were off by 2^-15 of the largest product.  The accumulators start at
 //           7 - m, m the running maximum: what comes out is the exponent of 2^7 p, and nothing is left to do but exp2.
-//   p . v   values are converted to f16 (exact), probabilities to f16 too: v_mfma_f32_*_f16.
+//   p . v   bf16 rows: values are converted to f16 (exact), probabilities to f16 too: v_mfma_f32_*_f16.  f32 rows: values and three
+//           terms of each probability in bf16, all exact: v_mfma_f32_*_bf16.
 //
 // Two kernels.  Requests of few rows: a wave takes 16 rows and a share of the keys, bytes of the cache go from memory to
 // registers (cache_few_kernel); short requests are not cut, or by the waves of a workgroup only.  Others: four waves of 32 rows share tiles in LDS, whose values are converted
@@ -36,6 +37,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
 // (token, head) rows of a request past which it goes to cache_many_kernel.  The two cross between 48 and 64 against 4,096 tokens
@@ -60,7 +62,9 @@ constexpr float kFewJoin = 1.f / 512, kManyJoin = 1.f / 32;   // what writing an
 constexpr int kSlackPieces = 64;                // the pages of a piece are formed in f32
 // "Pages of a piece" where no tile is cut: a tile is a wave's, or (few rows) a workgroup's.
 constexpr int kWave = 1 << 30, kWhole = INT_MAX;
-constexpr float kShift = 7.0f;   // probabilities are held as 2^7 p: f16 keeps all bits down to 2^-21 of the maximum's
+// Probabilities are held as 2^7 p: f16 keeps all bits down to 2^-21 of the maximum's, and ends at 2^-31.  Further down with a higher start
+// (2^14, and 2^15.5 for kMost) the maximum is raised more often: causal prefills 6 to 8% slower (d = 64, 2,048 rows over 6,144 tokens 150 and 160 us).
+constexpr float kShift = 7.0f;
 constexpr float kMost = 15.0f;   // exponent past which the running maximum is raised: 2^15 < 65504
 constexpr float kLowest = -3.402823466e38f;
 
@@ -409,12 +413,13 @@ __device__ __forceinline__ void store_run(void* out, long long at, f32x4 v, int 
     }
 }
 
-// Eight f16 values (keys) of each channel of a lane's bytes, BYTES bytes (two channels each) a key.  scale[k]: exponent of key k, as a
-// float of which the conversion reads the exponent only.
-template <int BYTES>
-__device__ __forceinline__ void values_f16(const uint32_t* v, const float (&scale)[8], f16x8* out) {
-#define SOL_CVT(w, s, sel) __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, sel))
-    u32x4 r[2 * BYTES];
+// Eight values (keys) of each channel of a lane's bytes, BYTES bytes (two channels each) a key, in f16 or bf16 (F32T), both exact.
+// scale[k]: exponent of key k, as a float of which the conversion reads the exponent only.
+template <int BYTES, bool F32T>
+__device__ __forceinline__ void values_of(const uint32_t* v, const float (&scale)[8], u32x4* out) {
+#define SOL_CVT(w, s, sel)                                                                         \
+    (F32T ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, sel))     \
+          : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, sel)))
 #pragma unroll
     for (int j = 0; j < 4; ++j) {   // keys 2j, 2j + 1
 #pragma unroll
@@ -427,12 +432,10 @@ __device__ __forceinline__ void values_f16(const uint32_t* v, const float (&scal
                 x = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j], 2) : SOL_CVT(v[j >> 1], scale[2 * j], 0);
                 y = j & 1 ? SOL_CVT(v[j >> 1], scale[2 * j + 1], 3) : SOL_CVT(v[j >> 1], scale[2 * j + 1], 1);
             }
-            r[2 * b][j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-            r[2 * b + 1][j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            out[2 * b][j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            out[2 * b + 1][j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
     }
-#pragma unroll
-    for (int c = 0; c < 2 * BYTES; ++c) out[c] = __builtin_bit_cast(f16x8, r[c]);
 #undef SOL_CVT
 }
 
@@ -443,16 +446,48 @@ __device__ __forceinline__ void scales_of(uint32_t b, float* scale) {
     scale[3] = __uint_as_float(b >> 1);
 }
 
-// Probabilities as f16 operands, rounded to nearest (F32T: two terms), and their sum, in f32, added to l.  (A sum of the rounded ones by
-// v_dot2_f32_f16 takes half the instructions, but they do not run beside those of the matrix cores.)
+// Probabilities of eight keys as operands of the second product: f16, rounded to nearest, or for f32 rows three bf16 terms that hold
+// all bits of an f32 at any size.  (Two f16 terms lose those of small ones: beside a token that stands 22 nats above all others
+// and whose value is 0, outputs were off by 1e-2 to 1e-1.  2,048 f32 rows over 6,144 tokens, 32 heads: 400 us with them, 470 with three.)
 template <bool F32T>
-__device__ __forceinline__ void cut_pair(float e0, float e1, f16x8& hi, f16x8& lo, int i, float& l) {
-    const f16x2 h = {(_Float16)e0, (_Float16)e1};
-    hi[2 * i] = h[0], hi[2 * i + 1] = h[1];
+struct Probs {
+    u32x4 w[F32T ? 3 : 1];
+};
+
+// Keys 2i and 2i + 1 of them; their sum, in f32, is added to l.  (A sum of the rounded ones by v_dot2_f32_f16 takes half the
+// instructions, but they do not run beside those of the matrix cores.)
+template <bool F32T>
+__device__ __forceinline__ void cut_pair(float e0, float e1, Probs<F32T>& p, int i, float& l) {
     l += e0;
     l += e1;
     if constexpr (F32T) {
-        lo[2 * i] = (_Float16)(e0 - (float)h[0]), lo[2 * i + 1] = (_Float16)(e1 - (float)h[1]);
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {   // each takes the upper eight significant bits of what is left
+            const uint32_t b0 = __float_as_uint(e0), b1 = __float_as_uint(e1);
+            p.w[t][i] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+            e0 -= __uint_as_float(b0 & 0xffff0000u);
+            e1 -= __uint_as_float(b1 & 0xffff0000u);
+        }
+    } else {
+        p.w[0][i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)e0, (_Float16)e1});
+    }
+}
+
+// o + v p, on 16 x 16 x 32 or 32 x 32 x 16 tiles.
+template <bool F32T, class O>
+__device__ __forceinline__ void add_values(const u32x4& v, const Probs<F32T>& p, O& o) {
+    constexpr bool SMALL = sizeof(O) == sizeof(f32x4);
+    if constexpr (F32T) {
+#pragma unroll
+        for (int t = 2; t >= 0; --t) {
+            const bf16x8 a = __builtin_bit_cast(bf16x8, v), b = __builtin_bit_cast(bf16x8, p.w[t]);
+            if constexpr (SMALL) o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, o, 0, 0, 0);
+            else o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, o, 0, 0, 0);
+        }
+    } else {
+        const f16x8 a = __builtin_bit_cast(f16x8, v), b = __builtin_bit_cast(f16x8, p.w[0]);
+        if constexpr (SMALL) o = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, o, 0, 0, 0);
+        else o = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, o, 0, 0, 0);
     }
 }
 
@@ -620,12 +655,12 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
     }
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-        f16x8 ph = {}, pl = {};
+        Probs<F32T> p = {};
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                cut_pair<F32T>(__builtin_amdgcn_exp2f(s[2 * w + b][2 * e]), __builtin_amdgcn_exp2f(s[2 * w + b][2 * e + 1]), ph, pl, 2 * b + e, l);
+                cut_pair<F32T>(__builtin_amdgcn_exp2f(s[2 * w + b][2 * e]), __builtin_amdgcn_exp2f(s[2 * w + b][2 * e + 1]), p, 2 * b + e, l);
         float vs[8];
         scales_of(pg.vs[w][0], vs);
         scales_of(pg.vs[w][1], vs + 4);
@@ -638,18 +673,15 @@ __device__ __forceinline__ void few_second(const FewPage<D>& pg, f32x4 (&s)[4], 
         for (int c = 0; c < D / 64; ++c) {
             // 16 bytes: eight keys of two bytes (d = 128), or two runs of eight bytes (d = 64)
             const uint32_t bytes[4] = {pg.v[w][c][0], pg.v[w][c][1], pg.v[w][c][2], pg.v[w][c][3]};
-            f16x8 va[4];
+            u32x4 va[4];
             if constexpr (D == 128) {
-                values_f16<2>(bytes, vs, va);
+                values_of<2, F32T>(bytes, vs, va);
             } else {
-                values_f16<1>(bytes, vs, va);
-                values_f16<1>(bytes + 2, vs, va + 2);
+                values_of<1, F32T>(bytes, vs, va);
+                values_of<1, F32T>(bytes + 2, vs, va + 2);
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                o[4 * c + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[t], ph, o[4 * c + t], 0, 0, 0);
-                if constexpr (F32T) o[4 * c + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[t], pl, o[4 * c + t], 0, 0, 0);
-            }
+            for (int t = 0; t < 4; ++t) add_values(va[t], p, o[4 * c + t]);
         }
     }
 }
@@ -822,7 +854,7 @@ __device__ __forceinline__ int swap23(int i) { return (i & 19) | ((i & 4) << 1) 
 template <int D>
 struct Stage {
     u32x4 k[2 * (D / 64) * 64];     // [window][64-channel chunk][lane]
-    f16x8 v[4 * (D / 32) * 64];     // [16-key step][channel tile][lane]
+    u32x4 v[4 * (D / 32) * 64];     // [16-key step][channel tile][lane]
     uint32_t ks[64];                // scale bytes [chunk][window] of a lane
 };
 
@@ -856,7 +888,7 @@ __device__ __forceinline__ void many_load(const uint8_t* page, ManyPage<D>& r) {
 }
 
 // left: tokens of the page that there are; what lies behind them may be anything, and a finite scale keeps 0 v = 0.
-template <int D>
+template <int D, bool F32T>
 __device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, int left) {
     constexpr int CT = D / 32;
     const int t = threadIdx.x;
@@ -872,8 +904,8 @@ __device__ __forceinline__ void many_store(const ManyPage<D>& r, Stage<D>& st, i
             if (8 * (t >> 5) + i >= left) vs[i] = 1.0f;
     }
     const uint32_t bytes[4] = {r.v[0], r.v[1], r.v[2], r.v[3]};
-    f16x8 va[CT];
-    values_f16<D / 64>(bytes, vs, va);
+    u32x4 va[CT];
+    values_of<D / 64, F32T>(bytes, vs, va);
 #pragma unroll
     for (int c = 0; c < CT; ++c) st.v[((t >> 6) * CT + c) * 64 + (t & 63)] = va[c];   // keys 16 (t >> 6) + 8 (t >> 5 & 1) ...
 }
@@ -940,17 +972,13 @@ __device__ __forceinline__ void many_page(const Stage<D>& st, const Split<F32T ?
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-        f16x8 ph = {}, pl = {};
+        Probs<F32T> p = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             cut_pair<F32T>(__builtin_amdgcn_exp2f(s[u >> 1][8 * (u & 1) + 2 * i]), __builtin_amdgcn_exp2f(s[u >> 1][8 * (u & 1) + 2 * i + 1]),
-                           ph, pl, i, l);
+                           p, i, l);
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            const f16x8 va = st.v[(u * CT + t) * 64 + lane];
-            o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, ph, o[t], 0, 0, 0);
-            if constexpr (F32T) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pl, o[t], 0, 0, 0);
-        }
+        for (int t = 0; t < CT; ++t) add_values(st.v[(u * CT + t) * 64 + lane], p, o[t]);
     }
     __builtin_amdgcn_s_setprio(0);
 }
@@ -1020,7 +1048,7 @@ __device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& p
     // the page of tokens key0 ... is in stage[turn], the one after it in registers
     int turn = 0, key0 = pages.p * kPage;
     if (more) {
-        many_store<D>(pg, stage[0], pc.len - key0);
+        many_store<D, F32T>(pg, stage[0], pc.len - key0);
         id = pages.next();
         if (id >= 0) many_load<D>(store + id * page_stride, pg);
     }
@@ -1030,7 +1058,7 @@ __device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& p
         more = id >= 0;
         if (more) {
             key0 = pages.p * kPage;
-            many_store<D>(pg, stage[turn ^ 1], pc.len - key0);
+            many_store<D, F32T>(pg, stage[turn ^ 1], pc.len - key0);
             id = pages.next();
             if (id >= 0) many_load<D>(store + id * page_stride, pg);
         }

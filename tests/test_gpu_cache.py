@@ -969,3 +969,47 @@ def test_forward_every_way_of_cutting(dev, dtype, d, Hq, Hk, S, rows, lens, part
             off, norm = off + float(err.square().sum()), norm + float(ref.square().sum())
     # over all values: as in test_forward_cut_into_pieces
     assert math.sqrt(off / norm) <= (2.0 ** -8 / math.sqrt(3) * 1.25 if dtype == "bf16" else 2.0 ** -20)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [1, 60])                   # both kernels
+@pytest.mark.parametrize("L,wide", [(700, 0), (3000, 0), (20000, 100)])
+@pytest.mark.parametrize("gap", [17, 22, 45])
+def test_forward_beside_a_token_of_nearly_all_the_weight(dev, dtype, d, rows, L, wide, gap):
+    """A token whose value is 0 stands `gap` nats above all others: what the others give is all that there is to see.
+
+    f32: as in tolerance(), with the error of each key's own logit, but no probability is too small to be exact: an exponential is off
+    by an ulp, which the 2^-22 of tolerance() holds.  bf16: as there, each is off by up to 2^-32 of the largest, an error on sum |v|."""
+    P = -(-L // 64)
+    g = torch.Generator(device=dev).manual_seed(L + gap)
+    k = 0.1 * torch.randn(1, P * 64, d, generator=g, device=dev)
+    v = torch.randn(1, P * 64, d, generator=g, device=dev) + 1.0
+    k[..., :32] = 0.0
+    k[0, L // 3], v[0, L // 3] = 0.0, 0.0
+    q = 0.25 * torch.randn(1, rows, d, generator=g, device=dev)
+    q[..., :32] = 0.0
+    k[0, L // 3, 0] = 3.0 * 2.0 ** round(math.log2(gap * math.sqrt(d) / 8.0 / 3.0))
+    q[..., 0] = gap * math.sqrt(d) / float(k[0, L // 3, 0])
+    q = q.to(DT[dtype])
+    store = sc.empty(P, 1, d, dev)
+    slots = torch.arange(P * 64, dtype=torch.int32, device=dev)
+    sc.append(k, v, store, slots)
+    table = torch.nn.functional.pad(torch.arange(P, dtype=torch.int32, device=dev)[None], (0, wide), value=-1)
+    out = sc.forward(q, store, table, i32([L], dev), i32([0, rows], dev), i32([L - 1] * rows, dev))
+    k, v = (x.double()[0, :L] for x in sc.read(store, slots, dtype=torch.float32))
+    q = q.double()[0]
+    s = (q @ k.T.contiguous()) / math.sqrt(d)
+    p = torch.softmax(s, -1)
+    assert bool((s[:, L // 3, None] - s >= gap - 2)[:, torch.arange(L, device=dev) != L // 3].all())
+    ref = p @ v
+    top = q.abs().unflatten(-1, (-1, 32)).amax(-1).repeat_interleave(32, -1)
+    lost = top * (2.0 ** -12 if dtype == "bf16" else 2.0 ** -24) / 3.75 + 2 * 2.0 ** -24 * q.abs()
+    size = (q.abs() @ k.abs().T.contiguous()) / math.sqrt(d)
+    ds = (lost @ k.abs().T.contiguous()) / math.sqrt(d) + d * 2.0 ** -24 * size + 4 * 2.0 ** -24 * (size.amax(-1, keepdim=True) + 16)
+    spread = ((p * ds)[..., None] * (v[None] - ref[:, None]).abs()).sum(1) if rows == 1 else ds.amax(-1, keepdim=True) * 2 * (p @ v.abs())
+    reach = p @ v.abs()
+    bound = (HALF_STEP[dtype] * 1.01 + 2.0 ** -23) * ref.abs() + 2 * spread + (L / 16 + 64) * 2.0 ** -24 * reach
+    bound += (2.0 ** -11 * reach + 2.0 ** -32 * v.abs().sum(0)) if dtype == "bf16" else 2.0 ** -22 * reach
+    err = (out[0].double() - ref).abs()
+    assert bool((err <= bound).all()), (float((err / bound).max()), float(err.norm() / ref.norm()))
