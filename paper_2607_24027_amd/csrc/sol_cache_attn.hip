@@ -307,6 +307,21 @@ __device__ __forceinline__ bool find_piece_shared(const CacheAttnArgs& a, const 
 // ---------------------------------------------------------------------------
 // Query rows: 32 channels of a lane's row, as terms of 6-bit floats.  Byte t of the scales is that of term t.
 // ---------------------------------------------------------------------------
+// The conversions write their results before they have read all of their operands, which the compiler does not know: it gives both the
+// same registers where it can, and the last term comes out wrong (errors of 3e-3 where 1.7e-3 is the rounding).  Hence results
+// marked as written early.  The compiler does not look for waits inside: what wrote the operands, and what reads the results, may
+// be neighbours, and two wait states on each side are as many as any vector instruction but the matrix ones asks for.
+__device__ __forceinline__ u32x6 to_6_bits(const f32x16& even, const f32x16& odd, float scale) {   // interleaves the two
+    u32x6 r;
+    asm("s_nop 1\n\tv_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3\n\ts_nop 1" : "=&v"(r) : "v"(even), "v"(odd), "v"(scale));
+    return r;
+}
+__device__ __forceinline__ f32x32 from_6_bits(const u32x6& x, float scale) {
+    f32x32 r;
+    asm("s_nop 1\n\tv_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 1" : "=&v"(r) : "v"(x), "v"(scale));
+    return r;
+}
+
 template <int NT>
 struct Split {
     u32x6 w[NT];
@@ -322,22 +337,18 @@ __device__ __forceinline__ Split<NT> split_row(const float (&x)[32]) {
     // the largest magnitude lies in (3.75, 7.5] 2^e
     int e = (int)((top + 0xfffffu) >> 23) - 127 - 2;
     e = min(max(e, -100), 125);
-    f32x16 even, odd;   // the conversion interleaves its two operands
+    f32x16 even, odd;
 #pragma unroll
     for (int i = 0; i < 16; ++i) even[i] = x[2 * i], odd[i] = x[2 * i + 1];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const uint32_t byte = e + 127 - 4 * t;
         const float scale = __uint_as_float(byte << 23);
-        r.w[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
-        // The instruction writes its result before it has read all of its operands, which the compiler does not know: used behind it,
-        // they cannot share registers with the result (which made the last term wrong: errors of 3e-3 where 1.7e-3 is the rounding).
-        asm("" : "+v"(r.w[t]) : "v"(even), "v"(odd), "v"(scale));
+        r.w[t] = to_6_bits(even, odd, scale);
         if (t % 4 == 0) r.scale[t / 4] = 0;
         r.scale[t / 4] |= byte << (8 * (t % 4));
         if (t + 1 < NT) {
-            f32x32 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.w[t], scale);
-            asm("" : "+v"(y) : "v"(r.w[t]), "v"(scale));   // likewise
+            const f32x32 y = from_6_bits(r.w[t], scale);
 #pragma unroll
             for (int i = 0; i < 16; ++i) even[i] -= y[2 * i], odd[i] -= y[2 * i + 1];
         }

@@ -2,6 +2,8 @@
 import ctypes
 import os
 import re
+import struct
+import subprocess
 
 import numpy as np
 import pytest
@@ -13,6 +15,7 @@ from paper_2607_24027_amd import cache as sc
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "sol_cache.h")
+OBJDUMP = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "llvm-objdump")
 P = ctypes.c_void_p
 A, B_, C, D_, E, F, G, H, I, J = (P(0x100000 * (i + 1)) for i in range(10))   # never dereferenced
 INVALID, UNSUPPORTED, WORKSPACE = sb.SOL_ERR_INVALID_ARG, sb.SOL_ERR_UNSUPPORTED, sb.SOL_ERR_WORKSPACE
@@ -257,3 +260,36 @@ def test_device_of_the_tensors_is_made_current_for_the_call(monkeypatch):
     assert calls == [("enter", other), (3, 101), ("exit", other)]
     with pytest.raises(sb.SolAttnError):
         sc._call(lambda *a: -1, torch.device("cuda", 0))
+
+
+def gfx950_objects(path):
+    """The gfx950 code objects of a shared library that hipcc linked."""
+    data = open(path, "rb").read()
+    magic, at, found = b"__CLANG_OFFLOAD_BUNDLE__", 0, []
+    while (at := data.find(magic, at)) >= 0:
+        entries, = struct.unpack_from("<Q", data, at + len(magic))
+        p = at + len(magic) + 8
+        for _ in range(entries if entries < 8 else 0):      # the library's own text may hold the word too
+            offset, size, n = struct.unpack_from("<QQQ", data, p)
+            if b"gfx950" in data[p + 24:p + 24 + n]:
+                found.append(data[at + offset:at + offset + size])
+            p += 24 + n
+        at += len(magic)
+    return found
+
+
+@pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="no llvm-objdump")
+def test_conversions_of_queries_keep_results_and_operands_apart(tmp_path):
+    """The conversions to and from 6-bit floats write their results before they have read all operands: in no kernel may the two
+    share registers."""
+    seen = 0
+    for i, code in enumerate(gfx950_objects(sb.LIB_PATH)):
+        path = tmp_path / f"{i}.o"
+        path.write_bytes(code)
+        text = subprocess.run([OBJDUMP, "-d", "--mcpu=gfx950", str(path)], capture_output=True, text=True, check=True).stdout
+        for line in re.findall(r"v_cvt_scalef32_(?:2xpk16_fp6_f32|pk32_f32_fp6)[^/\n]*", text):
+            regs = [set(range(int(a), int(b or a) + 1)) for a, b in re.findall(r"\bv\[?(\d+)(?::(\d+))?\]?", line.split(None, 1)[1])]
+            assert len(regs) >= 3 and not any(regs[0] & r for r in regs[1:]), line
+            seen += 1
+    # bf16 rows: three terms and two of them back, f32 six and five, for the blocks of 32 channels of a lane
+    assert seen >= 5 * 4 + 11 * 4, seen
