@@ -51,6 +51,7 @@ constexpr int kFewWaves = 4;                    // waves of a workgroup of cache
 constexpr int kFewSlots = 12 * 256;             // waves of it that the GPU holds, 12 a compute unit
 constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (three at d = 64 are slower)
 constexpr int kRounds = 7;                      // fillings of those slots at most (below 8: a lane for each of eight requests)
+constexpr int kManyRounds = 2;                  // past 64 requests, whose lanes hold several of them
 constexpr int kFewCost = 2, kManyCost = 20;     // what starting a piece and joining its result costs, in pages
 constexpr int kLeastPages = 2;                  // least pages of a piece
 constexpr int kRun = 16;                        // neighbouring pieces that a die gets in a row (an eighth of all: 17% slower on ragged requests)
@@ -136,6 +137,10 @@ __device__ __forceinline__ float wave_max(float x) {
     return at_lane(x, 63);
 }
 
+// Fillings of the slots at most that a plan is made for, of tiles that take up less than half of them or more.  The workspace has room
+// for no more.
+__host__ __device__ constexpr int most_rounds(int S, bool half) { return S > 64 ? kManyRounds : half ? kRounds : 1; }
+
 // Pages of a piece, at most, by which `tiles` tiles of `pages` pages in all become no more pieces than fill the slots k times.
 __device__ __forceinline__ int pages_for(float pages, float tiles, int slots, int k) {
     const float room = (float)slots * (float)k - tiles;   // each tile rounds up by one piece at most
@@ -145,7 +150,7 @@ __device__ __forceinline__ int pages_for(float pages, float tiles, int slots, in
 // Pages of a piece, at most: every tile of every request is cut into equal pieces of no more.  With few tiles, the pieces fill the slots
 // once; with many, it is chosen among fillings of one to kRounds times by the time that pieces dealt to free slots take, their
 // mean share and a quarter of a piece (half a piece and 12 pages a start: 2,048 rows over 6,144 tokens 300 us, 266 with these; 32
-// ragged requests 245, 260).  Past 64 requests (more loads for each lane) it is two fillings, or no cut at all.  By the
+// ragged requests 245, 260).  Past 64 requests (more loads for each lane) it is kManyRounds fillings, or no cut at all.  By the
 // lanes of one wave, on values that all waves of a launch see alike.  `planned`: the choice as another launch made it (not read
 // where it is quicker formed again than fetched from memory that another die wrote).  r: the lane's request, of up to 64.
 __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& part, const int* planned, Request& r) {
@@ -177,7 +182,7 @@ __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& pa
     if (!part.few && longest <= fminf(0.25f * tiles, 64.f)) return kWave;
     if (part.few && tiles >= kManyTiles && longest <= kWavePages) return kWave;
     if (part.few && longest <= fmaxf((float)part.whole, sum * (2.0f * kFewWaves / kFewSlots))) return kWhole;
-    int per = pages_for(sum, tiles, part.slots, a.S > 64 ? 2 : 1);
+    int per = pages_for(sum, tiles, part.slots, most_rounds(a.S, false));
     // Pieces of n pages make a join of pages / n shares, which it goes through in rounds of 16 of a row: the sum of n and the rounds
     // is least at the root (24 rows against 32,768 tokens of 8 heads: the call 34 us without this, 31 with it).  So is the sum of n and
     // the results of all pages / n pieces, 66 kB each of 128 rows (64 and 128 rows of 32 heads over 2,500 tokens: 31 and 35 us
@@ -1218,8 +1223,7 @@ long long most_tiles(const Part& part, int S, int T, int max_rows, int Hq, int H
 long long most_pieces(const Part& part, int S, int T, int max_rows, int Hq, int Hk, int max_pages) {
     const long long tiles = most_tiles(part, S, T, max_rows, Hq, Hk);
     if (part.uncut) return tiles;
-    // up to half the slots in tiles become one filling, more of them up to kRounds
-    const long long rounds = tiles > part.slots / 2 || S > 64 ? kRounds : 1;
+    const long long rounds = most_rounds(S, tiles > part.slots / 2);   // of no fewer tiles than there are
     return std::min(std::max(tiles, rounds * part.slots + kSlackPieces), tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
 }
 

@@ -293,3 +293,12 @@ def test_conversions_of_queries_keep_results_and_operands_apart(tmp_path):
             seen += 1
     # bf16 rows: three terms and two of them back, f32 six and five, for the blocks of 32 channels of a lane
     assert seen >= 5 * 4 + 11 * 4, seen
+
+
+@pytest.mark.parametrize("S", [64, 65, 300])
+def test_workspace_has_room_for_the_pieces_of_a_plan(S):
+    # single tokens, 32 and 8 heads of 128: 3,072 waves that the GPU holds, filled once for up to 64 requests and twice for more, or
+    # a piece for each tile where there are more tiles; 64 pieces of slack, 16 rows of 130 floats to a piece
+    tiles = (S * 4 // 16 + S) * 8
+    pieces = max(tiles, 3072 * (1 if S <= 64 else 2) + 64)
+    assert sc.workspace_bytes(S, S, 1, 32, 8, 128, 502) == 256 + pieces * 16 * 130 * 4
