@@ -88,6 +88,7 @@ struct Part {
     int whole;   // few rows: pages of the longest request up to which no tile is cut
     int uncut;   // kWave or kWhole where the table has no more, otherwise 0: a plan is formed
     bool few;    // the part of cache_few_kernel
+    unsigned room;   // results of pieces that the workspace holds
 };
 
 __device__ __forceinline__ Request request(const CacheAttnArgs& a, const Part& part, int s, int G) {
@@ -833,7 +834,7 @@ __device__ __forceinline__ void few_block(const CacheAttnArgs& a, const Part& pa
 #pragma unroll
             for (int t = 0; t < CT; t += 4)
                 store_run<F32T, VEC>(a.out, oi + CT * (4 * g + e) + t, f32x4{o[t][e], o[t + 1][e], o[t + 2][e], o[t + 3][e]} * inv, 4);
-    } else if (j < rows) {
+    } else if (j < rows && piece < part.room) {   // rows that overlap: no room was asked for
         float* to = ws->results + (long long)piece * (kFewTile * (D + 2));
         if (g == 0) to[2 * j] = m, to[2 * j + 1] = l;
         float* po = to + 2 * kFewTile + j * D;
@@ -1006,7 +1007,7 @@ struct ManySpace {
 };
 
 template <int D, bool F32T, bool VEC>
-__device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned piece, unsigned pieces,
+__device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& part, float scale_log2, PartSpace* ws, unsigned piece,
                                            ManySpace<D>& lds) {
     using L = PageLayout<D>;
     constexpr int NT = F32T ? 6 : 3, NC = D / 64, CT = D / 32;
@@ -1097,7 +1098,7 @@ __device__ __forceinline__ void many_piece(const CacheAttnArgs& a, const Part& p
         }
         return;
     }
-    if (slot >= pieces) return;   // rows that overlap: no room was asked for
+    if (slot >= part.room) return;   // rows that overlap: no room was asked for
     float* to = ws->results + (long long)slot * (kManyTile * (D + 2));
     const int row = 32 * wave + j;
     if (h == 0) to[2 * row] = most < 0.f ? kLowest : m, to[2 * row + 1] = l;
@@ -1112,7 +1113,7 @@ template <int D, bool F32T, bool VEC>
 __global__ __launch_bounds__(256, 2) void cache_many_kernel(const CacheAttnArgs a, const Part part, const float scale_log2,
                                                                                                        PartSpace* ws) {
     __shared__ ManySpace<D> lds;
-    many_piece<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x, gridDim.x, lds);
+    many_piece<D, F32T, VEC>(a, part, scale_log2, ws, blockIdx.x, lds);
 }
 
 // Both in one launch: the many first (their pieces are the longest), then the few, which fill what the last ones leave.
@@ -1126,7 +1127,7 @@ __global__ __launch_bounds__(256, 2) void cache_mixed_kernel(const CacheAttnArgs
         ManySpace<D> many;
         FewResults<D> few;
     } lds;
-    if (blockIdx.x < many_pieces) many_piece<D, F32T, VEC>(a, many, scale_log2, many_ws, blockIdx.x, many_pieces, lds.many);
+    if (blockIdx.x < many_pieces) many_piece<D, F32T, VEC>(a, many, scale_log2, many_ws, blockIdx.x, lds.many);
     else few_block<D, F32T, VEC>(a, few, scale_log2, few_ws, blockIdx.x - many_pieces, few_pieces, lds.few);
 }
 
@@ -1140,7 +1141,7 @@ constexpr int kJoinThreads = 512;
 struct JoinPart {
     Part part;
     PartSpace* ws;
-    unsigned pieces, tiles, per_tile;   // per_tile workgroups a tile, for `rows` rows each
+    unsigned tiles, per_tile;   // per_tile workgroups a tile, for `rows` rows each
     int rows;
 };
 
@@ -1157,7 +1158,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
     const unsigned block = blockIdx.x - (second ? head : 0);
     Piece pc;
     if (!find_piece_shared<true>(a, part, jp.ws, block / jp.per_tile, false, pc) || pc.chunks == 1) return;
-    if (pc.slot0 + (uint64_t)(pc.chunks - 1) * pc.tiles >= jp.pieces) return;   // rows that overlap: no room was asked for
+    if (pc.slot0 + (uint64_t)(pc.chunks - 1) * pc.tiles >= part.room) return;   // rows that overlap: no room was asked for
     const long long stride = (long long)pc.tiles * (part.tile * (D + 2));
     const float* const tile = jp.ws->results + (long long)pc.slot0 * (part.tile * (D + 2));
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -1219,12 +1220,11 @@ long long most_tiles(const Part& part, int S, int T, int max_rows, int Hq, int H
     return (rows / part.tile + requests) * Hk;
 }
 
-// Pieces at most: what fills the slots kRounds times, or one for each tile; and no tile has more than its pages give.
-long long most_pieces(const Part& part, int S, int T, int max_rows, int Hq, int Hk, int max_pages) {
-    const long long tiles = most_tiles(part, S, T, max_rows, Hq, Hk);
-    if (part.uncut) return tiles;
+// Pieces at most where tiles are cut: what fills the slots as often as a plan may; and no tile has more than its pages give.  More tiles
+// than that are not cut, and none leaves a result behind.
+long long most_cut(const Part& part, int S, long long tiles, int max_pages) {
     const long long rounds = most_rounds(S, tiles > part.slots / 2);   // of no fewer tiles than there are
-    return std::min(std::max(tiles, rounds * part.slots + kSlackPieces), tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
+    return std::min(rounds * part.slots + kSlackPieces, tiles * ((max_pages + kLeastPages - 1) / kLeastPages));
 }
 
 struct Plan {
@@ -1242,8 +1242,8 @@ Plan make_plan(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages)
     const long long most = (long long)std::min(max_rows, T) * (Hq / Hk);
     p.use_many = most > kFewRows && (max_pages > kShortPages || (long long)T * Hq > kShortRows);
     p.use_few = !p.use_many || S > 1;
-    p.few = {kFewTile, kFewSlots, kFewCost, 0, p.use_many ? kFewRows : INT_MAX, 0, 0, true};
-    p.many = {kManyTile, kManySlots, kManyCost, p.use_few ? kFewRows : 0, INT_MAX, 0, max_pages > kManyWhole ? 0 : kWave, false};
+    p.few = {kFewTile, kFewSlots, kFewCost, 0, p.use_many ? kFewRows : INT_MAX, 0, 0, true, 0};
+    p.many = {kManyTile, kManySlots, kManyCost, p.use_few ? kFewRows : 0, INT_MAX, 0, max_pages > kManyWhole ? 0 : kWave, false, 0};
     if (p.use_few) {
         const int rows = p.use_many ? std::min(max_rows, std::max(1, kFewRows / (Hq / Hk))) : max_rows;
         p.few_quads = (int)(std::min<long long>((long long)rows * (Hq / Hk), kFewTile) + 3) / 4;
@@ -1253,14 +1253,17 @@ Plan make_plan(int S, int T, int max_rows, int Hq, int Hk, int d, int max_pages)
         // tiles that there may be are up to half as many again as there are.
         p.few.whole = p.few_tiles >= 128 ? 32 : 16;
         if (max_pages <= p.few.whole) p.few.uncut = p.few_tiles >= kManyTiles / 2 * 3 && max_pages <= kWavePages ? kWave : kWhole;
-        p.few_pieces = most_pieces(p.few, S, T, rows, Hq, Hk, max_pages);
+        p.few.room = p.few.uncut ? 0 : (unsigned)most_cut(p.few, S, p.few_tiles, max_pages);
+        p.few_pieces = std::max<long long>(p.few_tiles, p.few.room);
         p.few_blocks = std::max(p.few_tiles, (p.few_pieces + kFewWaves - 1) / kFewWaves);
-        p.few_bytes = !p.few.uncut ? kPartHeader + (size_t)p.few_pieces * kFewTile * (d + 2) * sizeof(float) : 0;
+        p.few_bytes = !p.few.uncut ? kPartHeader + (size_t)p.few.room * kFewTile * (d + 2) * sizeof(float) : 0;
     }
     if (p.use_many) {
-        p.many_pieces = (most_pieces(p.many, S, T, max_rows, Hq, Hk, max_pages) / (8 * kRun) + 1) * 8 * kRun;   // whole turns of runs
+        auto turns = [](long long pieces) { return (pieces / (8 * kRun) + 1) * 8 * kRun; };   // whole turns of runs
         p.many_tiles = most_tiles(p.many, S, T, max_rows, Hq, Hk);
-        p.many_bytes = !p.many.uncut ? kPartHeader + (size_t)p.many_pieces * kManyTile * (d + 2) * sizeof(float) : 0;
+        p.many.room = p.many.uncut ? 0 : (unsigned)turns(most_cut(p.many, S, p.many_tiles, max_pages));
+        p.many_pieces = std::max<long long>(turns(p.many_tiles), p.many.room);
+        p.many_bytes = !p.many.uncut ? kPartHeader + (size_t)p.many.room * kManyTile * (d + 2) * sizeof(float) : 0;
     }
     return p;
 }
@@ -1294,12 +1297,12 @@ static hipError_t launch(const CacheAttnArgs& a, const Plan& p, hipStream_t st) 
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    JoinPart few{p.few, few_ws, (unsigned)p.few_pieces, few_ws ? (unsigned)p.few_tiles : 0u, (unsigned)p.few_quads, 4};
+    JoinPart few{p.few, few_ws, few_ws ? (unsigned)p.few_tiles : 0u, (unsigned)p.few_quads, 4};
     // Few tiles have many shares each: a workgroup then takes fewer of a tile's rows, down to four (64 rows against 32,768
     // tokens of 8 heads: the call 47 us with 32 rows to a workgroup, 34 with four).
     int rows = 32;
     while (rows > 4 && p.many_tiles * (kManyTile / rows) < 512) rows /= 2;
-    JoinPart many{p.many, many_ws, (unsigned)p.many_pieces, many_ws ? (unsigned)p.many_tiles : 0u, (unsigned)(kManyTile / rows), rows};
+    JoinPart many{p.many, many_ws, many_ws ? (unsigned)p.many_tiles : 0u, (unsigned)(kManyTile / rows), rows};
     if (const unsigned grid = few.tiles * few.per_tile + many.tiles * many.per_tile) {
         cache_join_kernel<D, F32T, VEC><<<grid, kJoinThreads, 0, st>>>(a, few, many);
         e = hipGetLastError();

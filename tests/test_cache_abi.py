@@ -302,3 +302,12 @@ def test_workspace_has_room_for_the_pieces_of_a_plan(S):
     tiles = (S * 4 // 16 + S) * 8
     pieces = max(tiles, 3072 * (1 if S <= 64 else 2) + 64)
     assert sc.workspace_bytes(S, S, 1, 32, 8, 128, 502) == 256 + pieces * 16 * 130 * 4
+
+
+def test_workspace_of_tiles_that_no_plan_cuts():
+    # 40 heads of a whole 720p video are 23,640 tiles of 128 rows: past 512 workgroups filled seven times they stay whole
+    at_most = 512 * 7 + 64
+    assert sc.workspace_bytes(1, 75600, 75600, 40, 40, 128, 1200) == 256 + -(-(at_most + 1) // 128) * 128 * 128 * 130 * 4
+    assert sc.workspace_bytes(1, 400000, 400000, 40, 40, 128, 7000) == sc.workspace_bytes(1, 75600, 75600, 40, 40, 128, 1200)
+    # single tokens of 4,000 requests of 64 heads: 272,000 tiles of 16 rows, 3,072 waves filled twice
+    assert sc.workspace_bytes(4000, 4000, 1, 64, 64, 64, 502) == 256 + (2 * 3072 + 64) * 16 * 66 * 4

@@ -1013,3 +1013,40 @@ def test_forward_beside_a_token_of_nearly_all_the_weight(dev, dtype, d, rows, L,
     bound += (2.0 ** -11 * reach + 2.0 ** -32 * v.abs().sum(0)) if dtype == "bf16" else 2.0 ** -22 * reach
     err = (out[0].double() - ref).abs()
     assert bool((err <= bound).all()), (float((err / bound).max()), float(err.norm() / ref.norm()))
+
+
+@pytest.mark.parametrize("Hq,Hk,S,rows,lens,most", [
+    (64, 8, 1, 7500, [7600], 2),             # 3,752 tiles of 128 rows, more than seven fillings of 512 workgroups
+    (70, 70, 100, 1, [3000, 100], 70),       # 7,000 tiles of 16 rows, more than two fillings of 3,072 waves
+    (8, 2, 150, 30, [3000, 200, 250], 2),    # both parts, cut
+])
+def test_forward_keeps_to_its_workspace(dev, Hq, Hk, S, rows, lens, most):
+    """A workspace of the very size, with other memory behind it; every request by itself gives the same to rounding."""
+    d = 64
+    g = torch.Generator(device=dev).manual_seed(S)
+    length = [lens[0]] + [lens[1 + s % (len(lens) - 1)] for s in range(S - 1)]
+    rows = [rows + 20 * (s % 3 == 0) * (S == 150) for s in range(S)]
+    held = [-(-n // 64) for n in length]
+    start, P, T = np.cumsum([0] + held), sum(held), sum(rows)
+    k, v = (torch.randn(Hk, P * 64, d, generator=g, device=dev) for _ in range(2))
+    store = sc.empty(P, Hk, d, dev)
+    sc.append(k, v, store, torch.arange(P * 64, dtype=torch.int32, device=dev))
+    table = torch.full((S, max(held) + 500), -1, dtype=torch.int32, device=dev)
+    for s in range(S):
+        table[s, :held[s]] = torch.arange(start[s], start[s + 1], dtype=torch.int32, device=dev)
+    q = torch.randn(T, Hq, d, generator=g, device=dev).transpose(0, 1)
+    row_start = np.cumsum([0] + rows)
+    positions = torch.cat([torch.arange(n - r, n, dtype=torch.int32, device=dev) for n, r in zip(length, rows)])
+    need = sc.workspace_bytes(S, T, max(rows), Hq, Hk, d, table.shape[1])
+    block = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device=dev)
+    out = sc.forward(q, store, table, i32(length, dev), i32(row_start, dev), positions, max_rows=max(rows), workspace=block[:need])
+    assert bool((block[need:] == 0x5A).all())
+    for s in [0, 1, S // 2, S - 1] if S > 1 else [0]:
+        at = slice(row_start[s], row_start[s + 1])
+        for h in range(0, Hk, most):
+            part = slice(h, h + most)
+            one = sc.forward(q[part.start * (Hq // Hk):part.stop * (Hq // Hk), at], store[:, part].contiguous(), table[s:s + 1],
+                             i32([length[s]], dev), i32([0, rows[s]], dev), positions[at].contiguous())
+            # f32: sums in another order, a rounding for 16 keys and 64 more on sum p |v| below the largest |v|
+            bound = 2 * (length[s] / 16 + 64 + 8) * 2.0 ** -24 * v.abs().amax()
+            assert bool(((one - out[part.start * (Hq // Hk):part.stop * (Hq // Hk), at]).abs() <= bound).all()), (s, h)
