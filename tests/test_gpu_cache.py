@@ -1050,3 +1050,48 @@ def test_forward_keeps_to_its_workspace(dev, Hq, Hk, S, rows, lens, most):
             # f32: sums in another order, a rounding for 16 keys and 64 more on sum p |v| below the largest |v|
             bound = 2 * (length[s] / 16 + 64 + 8) * 2.0 ** -24 * v.abs().amax()
             assert bool(((one - out[part.start * (Hq // Hk):part.stop * (Hq // Hk), at]).abs() <= bound).all()), (s, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("how", ["plain", "tokens", "odd"])
+@pytest.mark.parametrize("d,rot,B,N,Hq,Hk", [
+    (128, 128, 1, 3000, 37, 6),      # three heads to a workgroup: one has the last query head and two key heads, the last one has one
+    (128, 64, 2, 1000, 50, 25),      # four
+    (64, 32, 1, 9001, 21, 10),       # four, one with a query head and three key heads, the last one three
+    (64, 64, 3, 4000, 0, 33),        # keys only: six, the last one three
+    (128, 0, 1, 20000, 40, 3),       # sixteen, at most
+])
+def test_qk_norm_rope_several_heads_to_a_workgroup(dev, dtype, pairs, how, d, rot, B, N, Hq, Hk):
+    """Large calls: a workgroup goes through several heads, across the border of queries and keys."""
+    blocks = -(-B * N // (2048 // d))
+    assert min(blocks * (Hq + Hk) // 2048, Hq + Hk, 16) > 1
+    g = torch.Generator(device=dev).manual_seed(N)
+    P = N + 7
+    xs = [torch.randn(B, H, N, d, generator=g, device=dev).to(DT[dtype]) if H else None for H in (Hq, Hk)]
+    ws = [(1 + 0.3 * torch.randn(d, generator=g, device=dev)).to(DT[dtype]) if H else None for H in (Hq, Hk)]
+    angle = 7 * torch.rand(P, rot // 2, generator=g, device=dev, dtype=torch.float64)
+    cos, sin = (angle.cos().float(), angle.sin().float()) if rot else (None, None)
+    positions = torch.randint(0, P, (B, N), generator=g, device=dev, dtype=torch.int32)
+    positions[:, ::97] = -1
+    gpu = [None if x is None else placed(x, how, dev) for x in xs]
+    outs = [None if x is None else placed(torch.full_like(x, 7.0), how, dev) for x in xs]
+    got = sc.qk_norm_rope(*gpu, *ws, cos, sin, positions, interleaved=pairs, q_out=outs[0], k_out=outs[1])
+    there = (positions >= 0)[:, None, :, None]
+    for x, w, y in zip(xs, ws, got):
+        if x is None:
+            continue
+        ref = x.double()
+        ref = ref / (ref.square().mean(-1, keepdim=True) + 1e-6).sqrt() * w.double()
+        length = ref.abs()
+        if rot:
+            at = positions.clamp(min=0).long()
+            c, s = cos.double()[at][:, None], sin.double()[at][:, None]
+            half = rot // 2
+            ia, ib = (slice(0, rot, 2), slice(1, rot, 2)) if pairs else (slice(0, half), slice(half, rot))
+            a, b = ref[..., ia].clone(), ref[..., ib].clone()
+            ref[..., ia], ref[..., ib] = a * c - b * s, b * c + a * s
+            length[..., ia] = length[..., ib] = torch.hypot(a, b)
+        # as in test_qk_norm_rope
+        tol = HALF_STEP[dtype] * ref.abs() * (1 + 2.0 ** -7) + 24 * 2.0 ** -24 * length
+        assert bool(torch.where(there, (y.double() - ref).abs() <= tol, y == 7.0).all())
