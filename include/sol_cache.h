@@ -151,7 +151,7 @@ int sol_cache_read(const void* store, const int32_t* slots, void* k_out, void* v
  *   may run at the same time need different ones, and a captured graph keeps using the one
  *   it was captured with.  It may be NULL where 0 bytes are needed.
  * Logits, maxima and sums are f32.  q log2(e) / sqrt(d) is split into 6-bit floats for each channel: three (bf16), whose
- *   sum is off by at most 2^-12.9 of the largest magnitude of its 32 channels, or six (f32, 2^-24.9).  Probabilities are
+ *   sum is off by at most 2^-13.9 of the largest magnitude of its 32 channels, or six (f32, 2^-25.9).  Probabilities are
  *   f32 for f32 rows.  For bf16 rows they are rounded to f16, none to finer steps than 2^-31 of the row's largest, and their
  *   sum is taken before: a row of which one token has nearly all the weight shows what tokens of less than 2^-31 of that give
  *   to at most 2^-32 sum |v|.

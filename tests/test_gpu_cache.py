@@ -1095,3 +1095,33 @@ def test_qk_norm_rope_several_heads_to_a_workgroup(dev, dtype, pairs, how, d, ro
         # as in test_qk_norm_rope
         tol = HALF_STEP[dtype] * ref.abs() * (1 + 2.0 ** -7) + 24 * 2.0 ** -24 * length
         assert bool(torch.where(there, (y.double() - ref).abs() <= tol, y == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [3, 150])
+def test_forward_channels_beside_a_large_one(dev, dtype, d, rows):
+    """What the terms of a query leave of the other channels of a block whose largest one is 500 times as large (and meets keys of 0).
+
+    Of a top in (3.75, 7.5] the first term leaves up to 1/4, which is 4 to the second (steps of 1/4 from 2 on), that one up to
+    1/8, which is 2 to the third (steps of 1/8), and that one up to 1/16: three terms 2^-4 / 16^2, six 2^-4 / 16^5, of 3.75 at least.  Over all
+    values as in test_forward_every_term_of_the_queries: evenly spread, a logit's over sqrt(3) times the keys' root mean square."""
+    L = 4000
+    P = -(-L // 64)
+    g = torch.Generator(device=dev).manual_seed(d + rows)
+    k, v = (torch.randn(1, P * 64, d, generator=g, device=dev) for _ in range(2))
+    k[..., ::32] = 0.0
+    store = sc.empty(P, 1, d, dev)
+    slots = torch.arange(P * 64, dtype=torch.int32, device=dev)
+    sc.append(k, v, store, slots)
+    k, v = (x.double()[0, :L] for x in sc.read(store, slots, dtype=torch.float32))
+    q = torch.randn(2, rows, d, generator=g, device=dev)
+    q[..., ::32] = 500.0 + 24 * torch.rand(2, rows, d // 32, generator=g, device=dev)
+    q = q.to(DT[dtype])
+    table = torch.arange(P, dtype=torch.int32, device=dev)[None]
+    out = sc.forward(q, store, table, i32([L], dev), i32([0, rows], dev), i32([L - 1] * rows, dev)).double()
+    ref = torch.softmax((q.double().flatten(0, 1) @ k.T.contiguous()) / math.sqrt(d), -1) @ v
+    left = (2.0 ** -12 if dtype == "bf16" else 2.0 ** -24) / 3.75 * 524 * float(k.square().mean().sqrt())
+    parts = [left, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22, HALF_STEP[dtype] if dtype == "bf16" else 16 * 2.0 ** -24]
+    off = float((out.flatten(0, 1) - ref).norm() / ref.norm())
+    assert off <= math.sqrt(sum(x * x for x in parts) / 3), (off, left)
