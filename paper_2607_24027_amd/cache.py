@@ -133,15 +133,22 @@ def _check_ints(name, t, shape, device):
 
 
 def _overlap(a, b):
-    """Whether two tensors share memory, by their outermost bytes: False, or True where they may."""
+    """Whether two tensors share memory: False, or True where they may.  They do not if their outermost bytes lie apart, or if both
+    repeat with one stride, as parts of each row of one buffer do, and lie apart inside of it."""
     if a.device != b.device or not a.numel() or not b.numel():
         return False
+    dims = [[(st * t.element_size(), n) for st, n in zip(t.stride(), t.shape) if n > 1] for t in (a, b)]
 
-    def span(t):
-        last = sum(st * (n - 1) for st, n in zip(t.stride(), t.shape))
-        return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
-    (a0, a1), (b0, b1) = span(a), span(b)
-    return a0 < b1 and b0 < a1
+    def reach(t, steps):
+        return sum(st * (n - 1) for st, n in steps) + t.element_size()
+    a0, b0 = a.data_ptr(), b.data_ptr()
+    if a0 + reach(a, dims[0]) <= b0 or b0 + reach(b, dims[1]) <= a0:
+        return False
+    for period in {st for steps in dims for st, _ in steps if st}:
+        ra, rb = (reach(t, [(st, n) for st, n in steps if st % period]) for t, steps in zip((a, b), dims))
+        if (b0 - a0) % period >= ra and (a0 - b0) % period >= rb:
+            return False
+    return True
 
 
 def _disjoint(name, t, **others):

@@ -311,3 +311,54 @@ def test_workspace_of_tiles_that_no_plan_cuts():
     assert sc.workspace_bytes(1, 400000, 400000, 40, 40, 128, 7000) == sc.workspace_bytes(1, 75600, 75600, 40, 40, 128, 1200)
     # single tokens of 4,000 requests of 64 heads: 272,000 tiles of 16 rows, 3,072 waves filled twice
     assert sc.workspace_bytes(4000, 4000, 1, 64, 64, 64, 502) == 256 + (2 * 3072 + 64) * 16 * 66 * 4
+
+
+def test_overlap_of_views():
+    def cells(t):
+        at = torch.zeros((), dtype=torch.long)
+        for st, n in zip(t.stride(), t.shape):
+            at = at[..., None] + torch.arange(n) * st
+        return set(((t.data_ptr() + (at * t.element_size()).flatten()[:, None] + torch.arange(t.element_size())).flatten()).tolist())
+    rng = np.random.default_rng(0)
+    buffer = torch.zeros(4000)
+    apart = 0
+    for _ in range(3000):
+        views = []
+        for _ in range(2):
+            unit, rows = int(rng.choice([24, 48, 72])), int(rng.integers(1, 9))
+            heads, width = int(rng.integers(1, 4)), int(rng.integers(1, 9))
+            views.append(buffer.as_strided((rows, heads, width), (unit, int(rng.choice([8, 12])), 1), int(rng.integers(0, 100))))
+        if rng.random() < 0.3:
+            views[1] = views[1].view(torch.int32) if rng.random() < 0.5 else views[1].transpose(0, 1)
+        shared = bool(cells(views[0]) & cells(views[1]))
+        assert sc._overlap(*views) or not shared
+        apart += not sc._overlap(*views) and views[0].data_ptr() < views[1].data_ptr() + 4 * 24
+    assert apart > 100
+
+
+def test_outputs_may_lie_in_one_buffer():
+    """Parts of the rows of one buffer, as a projection's output has them: no output shares memory with another tensor."""
+    rows = torch.zeros(2, 10, 16, 64)                            # [B, N, 8 heads of q, 4 of k, 4 that are free, 64]
+    q, k, free = (rows[:, :, a:b].transpose(1, 2) for a, b in ((0, 8), (8, 12), (12, 16)))
+    other = torch.zeros(2, 10, 12, 64)
+    q_out, k_out = other[:, :, :8].transpose(1, 2), other[:, :, 8:].transpose(1, 2)
+    for call in (lambda: sc.qk_norm_rope(q, k, q_out=q_out, k_out=k_out), lambda: sc.qk_norm_rope(None, k, k_out=free)):
+        with pytest.raises(ValueError, match="GPU"):             # nothing else is wrong
+            call()
+    for call in (lambda: sc.qk_norm_rope(q, k, k_out=q[:, 4:]), lambda: sc.qk_norm_rope(q, k, q_out=q_out, k_out=q_out[:, 1:5])):
+        with pytest.raises(ValueError, match="overlap"):
+            call()
+    store, slots = torch.zeros(3, 4, 68 * 64, dtype=torch.uint8), torch.zeros(10, dtype=torch.int32)
+    kv = torch.zeros(10, 2, 4, 64).transpose(0, 2)               # [4, 2, 10, 64]
+    with pytest.raises(ValueError, match="GPU"):
+        sc.read(store, slots, k_out=kv[:, 0], v_out=kv[:, 1])
+    with pytest.raises(ValueError, match="overlap"):
+        sc.read(store, slots, k_out=kv[:, 0], v_out=kv[:, 0])
+    i32 = dict(dtype=torch.int32)
+    args = (store, torch.zeros(1, 2, **i32), torch.zeros(1, **i32), torch.zeros(2, **i32), torch.zeros(10, **i32))
+    with pytest.raises(ValueError, match="GPU"):
+        sc.forward(q[0], *args, out=torch.zeros(10, 16, 64)[:, :8].transpose(0, 1))
+    with pytest.raises(ValueError, match="GPU"):
+        sc.forward(q[0, :4], *args, out=free[0])
+    with pytest.raises(ValueError, match="overlap"):
+        sc.forward(q[0], *args, out=rows[0, :, 2:10].transpose(0, 1))

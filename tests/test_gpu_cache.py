@@ -1125,3 +1125,26 @@ def test_forward_channels_beside_a_large_one(dev, dtype, d, rows):
     parts = [left, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22, HALF_STEP[dtype] if dtype == "bf16" else 16 * 2.0 ** -24]
     off = float((out.flatten(0, 1) - ref).norm() / ref.norm())
     assert off <= math.sqrt(sum(x * x for x in parts) / 3), (off, left)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_in_one_buffer(dev, dtype):
+    """Outputs that are parts of the rows of one buffer hold what outputs of their own hold, and nothing between them is written."""
+    d, N, Hq, Hk = 128, 70, 6, 2
+    g = torch.Generator(device=dev).manual_seed(1)
+    q, k = (torch.randn(1, H, N, d, generator=g, device=dev).to(DT[dtype]) for H in (Hq, Hk))
+    buffer = torch.full((1, N, Hq + 2 * Hk, d), 3.0, dtype=DT[dtype], device=dev)
+    parts = [buffer[:, :, a:b].transpose(1, 2) for a, b in ((0, Hq), (Hq, Hq + Hk), (Hq + Hk, Hq + 2 * Hk))]
+    want = sc.qk_norm_rope(q, k)
+    sc.qk_norm_rope(q, k, q_out=parts[0], k_out=parts[1])
+    assert torch.equal(parts[0], want[0]) and torch.equal(parts[1], want[1]) and bool((parts[2] == 3.0).all())
+    store = sc.empty(2, Hk, d, dev)
+    slots = torch.arange(N, dtype=torch.int32, device=dev)
+    sc.append(want[1][0], k[0], store, slots)
+    held = sc.read(store, slots, dtype=DT[dtype])
+    sc.read(store, slots, k_out=parts[1][0], v_out=parts[2][0])
+    assert torch.equal(parts[1][0], held[0]) and torch.equal(parts[2][0], held[1]) and torch.equal(parts[0], want[0])
+    args = (store, i32([[0, 1]], dev), i32([N], dev), i32([0, N], dev), slots)
+    attn = sc.forward(want[0][0], *args)
+    sc.forward(want[0][0], *args, out=parts[0][0])
+    assert torch.equal(parts[0][0], attn) and torch.equal(parts[1][0], held[0]) and torch.equal(parts[2][0], held[1])
