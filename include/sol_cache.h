@@ -117,6 +117,8 @@ int sol_cache_tables(const int32_t* lens, const int32_t* add, int32_t* table, in
  *   e is kept in [-100, 125] for keys and in [-23, 13] for values, so that values are exact in
  *   f16 (magnitudes up to 49152, as the range contract of the bf16 forward asks; larger
  *   ones are held as 49152).  Codes are rounded to nearest, ties to the even code, 6 the largest.
+ *   Normal keys and values are off by 11 % (root mean square), attention's outputs over them by 16 % where logits have a standard
+ *   deviation of 1, by 25 % where it is 2.
  * A token with an infinity or NaN in the key or the value of a head is held there as NaN: every
  *   row that sees it is NaN, and no other row is.
  */
