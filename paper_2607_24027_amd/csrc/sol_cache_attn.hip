@@ -41,7 +41,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kFewTile = 16, kManyTile = 128;   // query rows of a piece
 // (token, head) rows of a request past which it goes to cache_many_kernel.  The two cross between 48 and 64 against 4,096 tokens
-// (8 requests: 24, 32, 48 and 64 rows 30, 30, 35 and 41 us on the few, 33, 33, 38 and 39 on the many), f32 at 48.
+// (8 requests: 24, 32, 48 and 64 rows 30, 30, 35 and 41 us on the few, 33, 33, 38 and 39 on the many), f32 past 64 (48 and 64 rows 44 and
+// 48 us on the few, 52 and 53 on the many).
 constexpr int kFewRows = 48;
 // With a table of no more pages and no more rows than that in all, every request is one of few rows: a workgroup for 16 rows fills the
 // GPU sooner (one and 8 requests of 64 tokens over 1,000, 32 heads: 22 and 38 us on the many, 10 and 25 on the few; 48 of them 73 and 88).
@@ -49,7 +50,7 @@ constexpr int kShortPages = 32, kShortRows = 16 * 1024;
 constexpr int kManyWhole = 8;                   // pages of a table up to which many rows are not cut
 constexpr int kFewWaves = 4;                    // waves of a workgroup of cache_few_kernel
 constexpr int kFewSlots = 12 * 256;             // waves of it that the GPU holds, 12 a compute unit
-constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (three at d = 64 are slower)
+constexpr int kManySlots = 512;                 // workgroups of cache_many_kernel that it holds, two a compute unit (bf16 at d = 64 takes 158 registers and three run)
 constexpr int kRounds = 7;                      // fillings of those slots at most (below 8: a lane for each of eight requests)
 constexpr int kManyRounds = 2;                  // past 64 requests, whose lanes hold several of them
 constexpr int kFewCost = 2, kManyCost = 20;     // what starting a piece and joining its result costs, in pages
@@ -187,7 +188,7 @@ __device__ __forceinline__ int plan_pages(const CacheAttnArgs& a, const Part& pa
     // Pieces of n pages make a join of pages / n shares, which it goes through in rounds of 16 of a row: the sum of n and the rounds
     // is least at the root (24 rows against 32,768 tokens of 8 heads: the call 34 us without this, 31 with it).  So is the sum of n and
     // the results of all pages / n pieces, 66 kB each of 128 rows (64 and 128 rows of 32 heads over 2,500 tokens: 31 and 35 us
-    // without, 25 and 30 with it; f32, 48 requests of one row of 16 heads over 3,000: 33 and 27).
+    // without, 25 and 30 with it; f32, 48 requests of one row of 16 heads over 3,000: 35 and 28).
     per = max(per, (int)ceilf(sqrtf(fmaxf(longest * (1.0f / 16), sum * (part.few ? kFewJoin : kManyJoin)))));
     if (a.S <= 64 && tiles > 0.5f * (float)part.slots) {
         if (planned) return *planned;
@@ -860,7 +861,7 @@ __global__ __launch_bounds__(64 * kFewWaves, F32T && D == 128 ? 2 : 3) void cach
 // way.  Row i of a 32-key window is key i with bits 2 and 3 exchanged, so that the registers 8u ... 8u + 7 of the first
 // product are the eight consecutive keys that a lane holds of the second one's operand.
 //
-// Bound by what the matrix cores may draw: 3,600 rows of 40 heads over 75,600 tokens take 4.75 to 5.0 ms by the card, 1,110 to
+// Bound by what the matrix cores may draw: 3,600 rows of 40 heads over 75,600 tokens take 4.75 to 5.1 ms by the card, 1,090 to
 // 1,170 TFLOP/s at 1.9 GHz, where a large bf16 matrix product reaches 1,160.  The bare instructions of a page, on random data from
 // registers, take 0.77 us a wave and page whether one, two or three waves share a SIMD, on constant data 0.55; here it is 0.85.
 // That leaves nothing for an order of the loop: products of the next page before the sums of this one, a window at a time
