@@ -297,10 +297,10 @@ def test_conversions_of_queries_keep_results_and_operands_apart(tmp_path):
 
 @pytest.mark.parametrize("S", [64, 65, 300])
 def test_workspace_has_room_for_the_pieces_of_a_plan(S):
-    # single tokens, 32 and 8 heads of 128: 3,072 waves that the GPU holds, filled once for up to 64 requests and twice for more, or
+    # single tokens, 32 and 8 heads of 128: 12 waves on each of 256 compute units, filled once for up to 64 requests and twice for more, or
     # a piece for each tile where there are more tiles; 64 pieces of slack, 16 rows of 130 floats to a piece
     tiles = (S * 4 // 16 + S) * 8
-    pieces = max(tiles, 3072 * (1 if S <= 64 else 2) + 64)
+    pieces = max(tiles, 12 * 256 * (1 if S <= 64 else 2) + 64)
     assert sc.workspace_bytes(S, S, 1, 32, 8, 128, 502) == 256 + pieces * 16 * 130 * 4
 
 
@@ -309,8 +309,8 @@ def test_workspace_of_tiles_that_no_plan_cuts():
     at_most = 512 * 7 + 64
     assert sc.workspace_bytes(1, 75600, 75600, 40, 40, 128, 1200) == 256 + -(-(at_most + 1) // 128) * 128 * 128 * 130 * 4
     assert sc.workspace_bytes(1, 400000, 400000, 40, 40, 128, 7000) == sc.workspace_bytes(1, 75600, 75600, 40, 40, 128, 1200)
-    # single tokens of 4,000 requests of 64 heads: 272,000 tiles of 16 rows, 3,072 waves filled twice
-    assert sc.workspace_bytes(4000, 4000, 1, 64, 64, 64, 502) == 256 + (2 * 3072 + 64) * 16 * 66 * 4
+    # single tokens of 4,000 requests of 64 heads: 272,000 tiles of 16 rows, the waves filled twice
+    assert sc.workspace_bytes(4000, 4000, 1, 64, 64, 64, 502) == 256 + (2 * 12 * 256 + 64) * 16 * 66 * 4
 
 
 def test_overlap_of_views():

@@ -1017,7 +1017,7 @@ def test_forward_beside_a_token_of_nearly_all_the_weight(dev, dtype, d, rows, L,
 
 @pytest.mark.parametrize("Hq,Hk,S,rows,lens,most", [
     (64, 8, 1, 7500, [7600], 2),             # 3,752 tiles of 128 rows, more than seven fillings of 512 workgroups
-    (70, 70, 100, 1, [3000, 100], 70),       # 7,000 tiles of 16 rows, more than two fillings of 3,072 waves
+    (70, 70, 100, 1, [3000, 100], 70),       # 7,000 tiles of 16 rows, more than two fillings of the GPU
     (8, 2, 150, 30, [3000, 200, 250], 2),    # both parts, cut
 ])
 def test_forward_keeps_to_its_workspace(dev, Hq, Hk, S, rows, lens, most):
