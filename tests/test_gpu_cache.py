@@ -1148,3 +1148,44 @@ def test_outputs_in_one_buffer(dev, dtype):
     attn = sc.forward(want[0][0], *args)
     sc.forward(want[0][0], *args, out=parts[0][0])
     assert torch.equal(parts[0][0], attn) and torch.equal(parts[1][0], held[0]) and torch.equal(parts[2][0], held[1])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("rows", [3, 90])
+@pytest.mark.parametrize("wide", [0, 60])
+def test_forward_takes_values_as_clamped(dev, dtype, d, rows, wide):
+    """Lengths and rows that say too much are taken as clamped; positions past the length see all there is."""
+    rng = np.random.default_rng(rows)
+    store, _, _ = make_store(rng, 12, 2, d, dev)
+    table = np.pad(rng.permutation(12).reshape(3, 4), ((0, 0), (0, wide)), constant_values=-1)
+    T, room = 2 * rows + 4, 64 * (4 + wide)
+    q = torch.randn(6, T, d, generator=torch.Generator().manual_seed(rows)).to(DT[dtype]).to(dev)
+    positions = np.concatenate([np.arange(rows), np.arange(rows) + 150, [0, (1 << 31) - 1, -(1 << 31), 999]])
+    bad = sc.forward(q, store, i32(table, dev), i32([-(1 << 31), (1 << 31) - 1, 1 << 20], dev), i32([-9, rows, 2 * rows, (1 << 31) - 1], dev),
+                     i32(positions, dev), causal_granule=7)
+    good = sc.forward(q, store, i32(table, dev), i32([0, room, room], dev), i32([0, rows, 2 * rows, T], dev),
+                      i32(np.clip(positions, -1, room), dev), causal_granule=7)
+    assert torch.equal(bad, good) and bool(torch.isfinite(good).all())
+    assert bool((good[:, :rows] == 0).all()) and bool((good[:, T - 2] == 0).all()) and bool((good[:, T - 3] != 0).any())
+    # rows that end before they start are none, and leave what is there
+    out = torch.full_like(q, 5.0)
+    sc.forward(q, store, i32(table, dev), i32([200] * 3, dev), i32([T, 2, 1, 0], dev), i32(np.clip(positions, 0, 199), dev), out=out)
+    assert bool((out == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [2, 100])
+def test_forward_pages_twice_and_queries_without_strides(dev, dtype, rows):
+    """A page that a request's table names twice is there twice; one query for all heads, one for all tokens."""
+    d = 128
+    rng = np.random.default_rng(rows)
+    store, _, _ = make_store(rng, 3, 2, d, dev)
+    copied = torch.cat([store, store[1:2], store[1:2]])
+    g = torch.Generator().manual_seed(rows)
+    lens, row_start, positions = i32([300], dev), i32([0, rows], dev), i32([299] * rows, dev)
+    heads = torch.randn(1, rows, d, generator=g).to(DT[dtype]).to(dev).expand(8, rows, d)
+    tokens = torch.randn(8, 1, d, generator=g).to(DT[dtype]).to(dev).expand(8, rows, d)
+    for q in (heads, tokens):
+        twice = sc.forward(q, store, i32([[1, 0, 1, 2, 1]], dev), lens, row_start, positions)
+        apart = sc.forward(q.contiguous(), copied, i32([[1, 0, 3, 2, 4]], dev), lens, row_start, positions)
+        assert torch.equal(twice, apart)
